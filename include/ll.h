@@ -278,6 +278,73 @@ int ll_batch_dbg_get_logits(int32_t slot, float *host_out);
 int ll_batch_dbg_force_next_token(int32_t slot, int32_t tok);
 int ll_batch_dbg_time_steps(int32_t k, float *ms_out);
 
+/* ---- a key/value cache held in 4 bits ----
+ *
+ * Five bits an element instead of sixteen: a group of 32 consecutive elements of one head's key or value row is held as 32
+ * codes c in 0 .. 15 and two binary16 numbers s and mid, and stands for mid + s (c - 8).  s is the smallest binary16 number of
+ * at most 8 significant bits with 15 s >= max - min of the group, mid = min + 8 s rounded to binary16, c - 8 the element's
+ * distance from mid in steps of s, rounded to the nearest (half to even) and cut to -8 .. 7.  An element is off by at most
+ * s / 2 and mid's own rounding.  A group that holds a NaN or an infinity, or spans more than 122400, reads as NaN throughout.
+ *
+ * The three calls below work on one layer's pool, with or without an initialised instance, on the stream that they are given
+ * (a hipStream_t; NULL: the default stream) of the current device, which the memory has to belong to.  They return when their
+ * kernels are queued, hold no state between calls, allocate nothing, and can be captured into a graph.  Every pointer is a
+ * DEVICE pointer and stays the caller's.  ll_batch_open_kv runs batched decoding on such pools.
+ * Errors as above: LL_E_BAD_ARG, LL_E_BAD_CONFIG (a shape that is not supported), LL_E_WORKSPACE (pool or workspace too small
+ * or misaligned), LL_E_HIP; but for LL_E_HIP nothing was queued. */
+enum { LL_F16 = 0, LL_BF16 = 1 }; /* type of the rows at the calls' borders: binary16, bfloat16 */
+
+/* One layer's keys and values.  Regions [K codes][V codes][K parameters][V parameters], each padded to 256 bytes, with R =
+ * page_tokens * n_pages pool rows: codes [n_kv_heads][R][head_dim / 2], element 2 j of a row in the low half of byte j;
+ * parameters [n_kv_heads][R][head_dim / 32][s, mid].  Rows that were never written may hold anything.
+ * LL_E_BAD_CONFIG unless head_dim is 64 or 128, n_kv_heads, page_tokens and n_pages are at least 1 and R <= 2^26. */
+typedef struct {
+  void *pool; /* 256-byte aligned */
+  size_t pool_bytes;
+  int32_t n_kv_heads, head_dim, page_tokens, n_pages;
+} ll_kv4_cache;
+
+/* The rows of a call.  Sequence b (0 <= b < n_seqs) has rows row_start[b] .. row_start[b + 1] - 1, or max_rows rows from row
+ * b * max_rows on where row_start is NULL.  They are the last rows of a sequence of len[b] positions: the last one sits at
+ * position len[b] - 1.  Rows in front of position 0 have no place in the cache, rows outside every sequence are not touched,
+ * and of a sequence with more than max_rows rows the first max_rows are looked at.  page_table[b][i] (table_stride entries a
+ * sequence) is the first pool row of positions i * page_tokens ..: an entry that does not leave a whole page inside the pool,
+ * for instance a negative one, is a page that is not there, and so are positions beyond the table.  Two sequences may share
+ * pages that they only read. */
+typedef struct {
+  const int32_t *row_start;  /* [n_seqs + 1] or NULL */
+  const int32_t *len;        /* [n_seqs] */
+  const int32_t *page_table; /* [n_seqs][table_stride] */
+  int32_t n_seqs, max_rows, n_rows, table_stride;
+  int32_t max_len; /* about the longest len: how finely attention is cut into workgroups; 0: what the table holds */
+} ll_kv4_rows;
+
+/* [n_rows][heads][head_dim] of LL_F16 or LL_BF16, the last dimension contiguous; strides in elements.  Fastest where the
+ * address and both strides are multiples of 16 bytes. */
+typedef struct {
+  void *data;
+  int64_t row_stride, head_stride;
+} ll_kv4_view;
+
+/* Bytes of a pool; 0 for a shape that is not supported (pool and pool_bytes are not looked at). */
+size_t ll_kv4_pool_bytes(const ll_kv4_cache *cache);
+/* Quantises the rows of k and v into the cache.  Rows whose page is not there are dropped. */
+int ll_kv4_write(const ll_kv4_cache *cache, const ll_kv4_rows *rows, int32_t dtype, const ll_kv4_view *k, const ll_kv4_view *v,
+                 void *hip_stream);
+/* The same rows out of the cache into k and v.  Rows that are not there are zeros. */
+int ll_kv4_read(const ll_kv4_cache *cache, const ll_kv4_rows *rows, int32_t dtype, const ll_kv4_view *k, const ll_kv4_view *v,
+                void *hip_stream);
+/* Bytes of workspace ll_kv4_attention() needs for such a call (0: none, or arguments that it would reject). */
+size_t ll_kv4_attention_workspace_bytes(const ll_kv4_cache *cache, const ll_kv4_rows *rows, int32_t n_heads);
+/* Causal attention of the rows of q [n_rows][n_heads][head_dim] over their sequences' cached positions, the row's own among
+ * them; n_heads / n_kv_heads query heads in a row share a key head.  Scores are multiplied by scale (0: 1 / sqrt(head_dim)).
+ * k and v (both NULL, or both given) are the same rows' keys and values: they are written to the cache first, as by
+ * ll_kv4_write, and attended as they are held.  Rows that see no position give zeros.  out must not overlap q, k or v.
+ * workspace (256-byte aligned) holds nothing between calls; calls that may run at the same time need one each. */
+int ll_kv4_attention(const ll_kv4_cache *cache, const ll_kv4_rows *rows, int32_t dtype, int32_t n_heads, float scale,
+                     const ll_kv4_view *q, const ll_kv4_view *k, const ll_kv4_view *v, const ll_kv4_view *out, void *workspace,
+                     size_t workspace_bytes, void *hip_stream);
+
 /* ---- measurement and test hooks (not part of the four-call contract) ---- */
 
 /* Most polls of one hand-off in the kernel that runs small models' decode steps, before the step is given up and redone by

@@ -22,6 +22,7 @@ LL_FLAG_PERSISTENT = 4
 LL_FLAG_PER_LENGTH_GRAPHS = 8
 LL_FLAG_FUSED_ATTN_OPROJ = 16
 LL_FLAG_LEAN_WORKSPACE = 32
+LL_F16, LL_BF16 = 0, 1
 LL_MODE_PERSISTENT_GRAPH, LL_MODE_MULTIKERNEL_GRAPH, LL_MODE_EAGER, LL_MODE_PER_LENGTH_GRAPHS = 0, 1, 2, 3
 KERNEL_CLASSES = ("embed", "qkv", "attn", "oproj", "gateup", "down", "lmhead", "sample")
 LAYER_KEYS = ("attn_norm", "wq", "wk", "wv", "wo", "ffn_norm", "w_gate", "w_up", "w_down")
@@ -29,6 +30,7 @@ LAYER_KEYS = ("attn_norm", "wq", "wk", "wv", "wo", "ffn_norm", "w_gate", "w_up",
 EXPORTS = ("ll_workspace_bytes", "ll_init", "ll_prefill", "ll_prefill_static", "ll_decode_step", "ll_decode_n", "ll_reset",
            "ll_set_sampling", "ll_shutdown", "ll_max_prompt", "ll_position", "ll_decode_mode", "ll_last_error", "ll_dbg_get_logits",
            "ll_batch_pool_bytes", "ll_batch_open", "ll_batch_add", "ll_batch_step", "ll_batch_remove", "ll_batch_close",
+           "ll_kv4_pool_bytes", "ll_kv4_write", "ll_kv4_read", "ll_kv4_attention_workspace_bytes", "ll_kv4_attention",
            "ll_batch_dbg_get_logits", "ll_batch_dbg_force_next_token", "ll_batch_dbg_time_steps",
            "ll_dbg_get_hidden", "ll_dbg_set_spin_limit", "ll_dbg_give_up_at", "ll_dbg_small_plan", "ll_dbg_graph_stats", "ll_dbg_gemm_plan", "ll_dbg_gemm_slice_count", "ll_dbg_tile_plan", "ll_dbg_batch_order", "ll_dbg_force_next_token", "ll_dbg_get_kv", "ll_dbg_profile_decode",
            "ll_dbg_time_decode", "ll_dbg_time_kernel_class", "ll_dbg_stream_copy", "ll_dbg_stream_read", "ll_dbg_poison_scratch", "ll_dbg_trace_decode")
@@ -47,6 +49,20 @@ class LLLayerWeights(C.Structure):
 class LLWeights(C.Structure):
     _fields_ = [("tok_emb", C.c_void_p), ("layers", C.POINTER(LLLayerWeights)),
                 ("final_norm", C.c_void_p), ("lm_head", C.c_void_p)]
+
+
+class LLKV4Cache(C.Structure):
+    _fields_ = [("pool", C.c_void_p), ("pool_bytes", C.c_size_t)] + \
+               [(k, C.c_int32) for k in ("n_kv_heads", "head_dim", "page_tokens", "n_pages")]
+
+
+class LLKV4Rows(C.Structure):
+    _fields_ = [(k, C.c_void_p) for k in ("row_start", "len", "page_table")] + \
+               [(k, C.c_int32) for k in ("n_seqs", "max_rows", "n_rows", "table_stride", "max_len")]
+
+
+class LLKV4View(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("row_stride", C.c_int64), ("head_stride", C.c_int64)]
 
 
 class LLError(RuntimeError):
@@ -143,6 +159,16 @@ def load():
     L.ll_dbg_stream_read.argtypes = [C.c_void_p, C.c_size_t, C.c_int32, C.c_void_p, C.POINTER(C.c_float)]
     L.ll_dbg_time_decode.restype = C.c_int
     L.ll_dbg_time_decode.argtypes = [C.c_int32, C.POINTER(C.c_float)]
+    cache, rows, view = C.POINTER(LLKV4Cache), C.POINTER(LLKV4Rows), C.POINTER(LLKV4View)
+    L.ll_kv4_pool_bytes.restype = C.c_size_t
+    L.ll_kv4_pool_bytes.argtypes = [cache]
+    for name in ("ll_kv4_write", "ll_kv4_read"):
+        getattr(L, name).restype = C.c_int
+        getattr(L, name).argtypes = [cache, rows, C.c_int32, view, view, C.c_void_p]
+    L.ll_kv4_attention_workspace_bytes.restype = C.c_size_t
+    L.ll_kv4_attention_workspace_bytes.argtypes = [cache, rows, C.c_int32]
+    L.ll_kv4_attention.restype = C.c_int
+    L.ll_kv4_attention.argtypes = [cache, rows, C.c_int32, C.c_int32, C.c_float] + [view] * 4 + [C.c_void_p, C.c_size_t, C.c_void_p]
     _lib = L
     return L
 
@@ -224,6 +250,121 @@ def ll_dbg_gemm_slice_count(N, K, nmat, rows, col):
 
 def ll_last_error():
     return load().ll_last_error().decode()
+
+
+# ---- a key/value cache held in 4 bits ----
+
+def ll_kv4_pool_bytes(n_kv_heads, head_dim, page_tokens, n_pages):
+    """Bytes of one layer's pool (host arithmetic, no GPU needed); 0 for a shape that is not supported."""
+    return int(load().ll_kv4_pool_bytes(C.byref(LLKV4Cache(None, 0, n_kv_heads, head_dim, page_tokens, n_pages))))
+
+
+class KV4Cache:
+    """One layer's pool, a contiguous uint8 CUDA tensor of ll_kv4_pool_bytes() bytes on a 256-byte border, and its shape."""
+
+    def __init__(self, pool, n_kv_heads, head_dim, page_tokens, n_pages):
+        if not pool.is_cuda or not pool.is_contiguous():
+            raise ValueError("the pool must be a contiguous CUDA tensor")
+        self.pool, self.n_kv_heads, self.head_dim = pool, n_kv_heads, head_dim
+        self.c = LLKV4Cache(pool.data_ptr(), pool.numel() * pool.element_size(), n_kv_heads, head_dim, page_tokens, n_pages)
+
+
+class KV4Rows:
+    """Which rows a call has: int32 CUDA tensors ``lens`` [n_seqs], ``page_table`` [n_seqs, pages] and, unless every sequence
+    has ``max_rows`` rows, ``row_start`` [n_seqs + 1]; see ll_kv4_rows in include/ll.h."""
+
+    def __init__(self, lens, page_table, max_rows=1, row_start=None, max_len=0):
+        import torch
+        for t in (lens, page_table) if row_start is None else (lens, page_table, row_start):
+            if t.dtype != torch.int32 or not t.is_contiguous() or t.device != lens.device or not t.is_cuda:
+                raise ValueError("lens, page_table and row_start must be contiguous int32 tensors of one CUDA device")
+        n = lens.shape[0]
+        if lens.dim() != 1 or page_table.dim() != 2 or page_table.shape[0] != n or \
+                (row_start is not None and row_start.shape != (n + 1,)):
+            raise ValueError("lens [n_seqs], page_table [n_seqs, pages] and row_start [n_seqs + 1] do not fit together")
+        self.lens, self.page_table, self.row_start = lens, page_table, row_start
+        self.c = LLKV4Rows(None if row_start is None else row_start.data_ptr(), lens.data_ptr(), page_table.data_ptr(),
+                           n, max_rows, 0, page_table.shape[1], max_len)
+
+
+def _kv4_view(t, name, cache, heads, like=None):
+    if t.dim() != 3 or t.shape[2] != cache.head_dim or (heads and t.shape[1] != heads):
+        raise ValueError("%s must be [rows, %s, %d]" % (name, heads or "heads", cache.head_dim))
+    if like is not None and (t.dtype != like.dtype or t.shape[0] != like.shape[0]):
+        raise ValueError("%s must have the other tensors' type and rows" % name)
+    if t.device != cache.pool.device or t.stride(2) != 1:
+        raise ValueError("%s must be on the pool's device with a contiguous last dimension" % name)
+    return LLKV4View(t.data_ptr(), t.stride(0), t.stride(1))
+
+
+def _kv4_type(t):
+    import torch
+    if t.dtype not in (torch.float16, torch.bfloat16):
+        raise ValueError("rows are float16 or bfloat16, not %s" % t.dtype)
+    return LL_F16 if t.dtype == torch.float16 else LL_BF16
+
+
+def _kv4_on(cache, rows, stream):
+    """A context with the stream to work on (None: the current one of the pool's device) and its device as torch's current
+    ones, so that what the call allocates belongs to them, and the stream's handle."""
+    import torch
+    if rows.lens.device != cache.pool.device:
+        raise ValueError("lens and page_table must be on the pool's device")
+    if stream is None:
+        stream = torch.cuda.current_stream(cache.pool.device)
+    return torch.cuda.stream(stream), C.c_void_p(stream.cuda_stream)
+
+
+def ll_kv4_write(cache, rows, k, v, stream=None):
+    """Quantises rows of k and v, [rows, n_kv_heads, head_dim] float16 or bfloat16, into the cache."""
+    kv, vv = _kv4_view(k, "k", cache, cache.n_kv_heads), _kv4_view(v, "v", cache, cache.n_kv_heads, k)
+    rows.c.n_rows = k.shape[0]
+    on, s = _kv4_on(cache, rows, stream)
+    with on:
+        _check(load().ll_kv4_write(C.byref(cache.c), C.byref(rows.c), _kv4_type(k), C.byref(kv), C.byref(vv), s))
+
+
+def ll_kv4_read(cache, rows, k=None, v=None, n_rows=0, dtype=None, stream=None):
+    """The rows out of the cache into k and v, or into new tensors of n_rows rows."""
+    import torch
+    on, s = _kv4_on(cache, rows, stream)
+    with on:
+        if k is None:
+            k, v = torch.empty(2, n_rows, cache.n_kv_heads, cache.head_dim, dtype=dtype, device=cache.pool.device)
+        kv, vv = _kv4_view(k, "k", cache, cache.n_kv_heads), _kv4_view(v, "v", cache, cache.n_kv_heads, k)
+        rows.c.n_rows = k.shape[0]
+        _check(load().ll_kv4_read(C.byref(cache.c), C.byref(rows.c), _kv4_type(k), C.byref(kv), C.byref(vv), s))
+    return k, v
+
+
+def ll_kv4_attention_workspace_bytes(cache, rows, n_heads, n_rows):
+    """Bytes of workspace of such an attention call (host arithmetic)."""
+    rows.c.n_rows = n_rows
+    return int(load().ll_kv4_attention_workspace_bytes(C.byref(cache.c), C.byref(rows.c), n_heads))
+
+
+def ll_kv4_attention(cache, rows, q, k=None, v=None, scale=0.0, out=None, workspace=None, stream=None):
+    """Causal attention of rows q [rows, heads, head_dim] over the cache; k and v: these rows' own, written first.
+    Without ``workspace`` (a CUDA tensor on a 256-byte border) the call takes one from torch's allocator where it needs any."""
+    import torch
+    qv = _kv4_view(q, "q", cache, 0)
+    kv = None if k is None else C.byref(_kv4_view(k, "k", cache, cache.n_kv_heads, None))
+    vv = None if v is None else C.byref(_kv4_view(v, "v", cache, cache.n_kv_heads, None))
+    for t in (k, v, out):
+        if t is not None and (t.dtype != q.dtype or t.shape[0] != q.shape[0]):
+            raise ValueError("q, k, v and out must have the same type and number of rows")
+    on, s = _kv4_on(cache, rows, stream)
+    with on:
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        nbytes = ll_kv4_attention_workspace_bytes(cache, rows, q.shape[1], q.shape[0])
+        if workspace is None and nbytes:
+            workspace = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
+        _check(load().ll_kv4_attention(C.byref(cache.c), C.byref(rows.c), _kv4_type(q), q.shape[1], scale, C.byref(qv), kv, vv,
+                                       C.byref(_kv4_view(out, "out", cache, q.shape[1])),
+                                       None if workspace is None else C.c_void_p(workspace.data_ptr()),
+                                       0 if workspace is None else workspace.numel() * workspace.element_size(), s))
+    return out
 
 
 class Session:

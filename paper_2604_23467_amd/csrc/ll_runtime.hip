@@ -25,6 +25,7 @@
 #include "prefill_tile.h"
 #include "decode_small.h"
 #include "batch_kernels.h"
+#include "kv4_kernels.h"
 
 // Scratch of ll_prefill_static(): the buffers a short prefill needs besides its inputs and outputs
 // (activations, per-token partial sums, logits, selection candidates, the staged prompt ids), for
@@ -2484,3 +2485,5 @@ int ll_dbg_time_decode(int32_t k, float* ms_out) {
 }
 
 }  // extern "C"
+
+#include "kv4_host.h"
