@@ -91,11 +91,37 @@ void kv4_launch_write(hipStream_t s, int32_t dtype, int head_dim, const Kv4Pool&
   });
 }
 
+// How attention is cut into workgroups: row blocks of 16 query rows, and shares of the keys where that leaves CUs idle
+struct Kv4Plan {
+  int row_blocks, splits;
+  int64_t works;               // (row block, key head, sequence)
+  size_t bytes;                // of workspace
+};
+Kv4Plan kv4_plan(const Kv4Pool& p, const Kv4Rows& r, int max_len, int head_dim, int heads) {
+  Kv4Plan a{};
+  a.row_blocks = (int)(((int64_t)r.max_rows * (heads / p.kv_heads) + KV4_FEW_ROWS - 1) / KV4_FEW_ROWS);
+  a.works = (int64_t)a.row_blocks * p.kv_heads * r.n_seqs;
+  const int64_t most = (int64_t)r.table_stride * p.page_tokens;
+  const int64_t len = max_len > 0 ? std::min<int64_t>(max_len, most) : most;
+  const int64_t rounds = (len + KV4_TILE * KV4_WAVES - 1) / (KV4_TILE * KV4_WAVES);      // of the four waves over the keys
+  const int64_t want = (2 * num_cus() + a.works - 1) / std::max<int64_t>(a.works, 1);
+  a.splits = (int)std::max<int64_t>(1, std::min<int64_t>({want, rounds / 4, 64}));
+  if (a.splits > 1) a.bytes = align_up((size_t)a.works * a.splits * 16 * (head_dim + 2) * sizeof(float));
+  return a;
+}
+
 void kv4_launch_attention(hipStream_t s, int32_t dtype, int head_dim, const Kv4Pool& p, const Kv4Rows& r, int heads, float scale,
-                          const Kv4View& q, const Kv4View& o) {
-  const dim3 grid(r.n_rows, (heads + 3) / 4);
+                          const Kv4View& q, const Kv4View* k, const Kv4View* v, const Kv4View& o, const Kv4Plan& a, float* part) {
   kv4_dispatch(dtype, head_dim, [&](auto t, auto hd) {
-    hipLaunchKernelGGL((kv4_attn_simple_kernel<decltype(t), decltype(hd)::value>), grid, dim3(256), 0, s, p, r, q, o, heads, scale);
+    using T = decltype(t);
+    constexpr int HD = decltype(hd)::value;
+    const dim3 grid((unsigned)(a.works * a.splits));
+    if (k && r.max_rows == 1)
+      hipLaunchKernelGGL((kv4_attn_few_kernel<T, HD, true>), grid, dim3(256), 0, s, p, r, q, o, *k, *v, heads, scale, a.splits, a.row_blocks, part);
+    else
+      hipLaunchKernelGGL((kv4_attn_few_kernel<T, HD, false>), grid, dim3(256), 0, s, p, r, q, o, q, q, heads, scale, a.splits, a.row_blocks, part);
+    if (a.splits > 1)
+      hipLaunchKernelGGL((kv4_join_kernel<T, HD>), dim3((unsigned)a.works), dim3(256), 0, s, p, r, o, heads, a.splits, a.row_blocks, part);
   });
 }
 
@@ -147,7 +173,11 @@ int ll_kv4_read(const ll_kv4_cache* cache, const ll_kv4_rows* rows, int32_t dtyp
 }
 
 size_t ll_kv4_attention_workspace_bytes(const ll_kv4_cache* cache, const ll_kv4_rows* rows, int32_t n_heads) {
-  return 0;
+  Kv4Pool p;
+  Kv4Rows r;
+  if (kv4_check_cache("ll_kv4_attention_workspace_bytes", cache, false, &p) != LL_OK ||
+      kv4_check_rows("ll_kv4_attention_workspace_bytes", rows, false, &r) != LL_OK || n_heads < 1 || n_heads % p.kv_heads) return 0;
+  return kv4_plan(p, r, rows->max_len, cache->head_dim, n_heads).bytes;
 }
 
 int ll_kv4_attention(const ll_kv4_cache* cache, const ll_kv4_rows* rows, int32_t dtype, int32_t n_heads, float scale,
@@ -169,10 +199,18 @@ int ll_kv4_attention(const ll_kv4_cache* cache, const ll_kv4_rows* rows, int32_t
       (rc = kv4_check_view(who, "out", out, rows, n_heads, cache->head_dim, true, &oo)) != LL_OK) return rc;
   if (k && ((rc = kv4_check_view(who, "k", k, rows, p.kv_heads, cache->head_dim, false, &kk)) != LL_OK ||
             (rc = kv4_check_view(who, "v", v, rows, p.kv_heads, cache->head_dim, false, &vv)) != LL_OK)) return rc;
+  const Kv4Plan a = kv4_plan(p, r, rows->max_len, cache->head_dim, n_heads);
+  if (a.works * a.splits >= 1 << 24)
+    return fail(LL_E_BAD_ARG, "%s: %lld workgroups, a launch holds %d", who, (long long)(a.works * a.splits), (1 << 24) - 1);
+  if (workspace_bytes < a.bytes || (a.bytes && !workspace))
+    return fail(LL_E_WORKSPACE, "%s: workspace has %zu bytes, %zu needed", who, workspace_bytes, a.bytes);
+  if (a.bytes && reinterpret_cast<uintptr_t>(workspace) % kAlign)
+    return fail(LL_E_WORKSPACE, "%s: workspace must be %zu-byte aligned", who, kAlign);
   const hipStream_t s = static_cast<hipStream_t>(hip_stream);
-  if (k) kv4_launch_write(s, dtype, cache->head_dim, p, r, kk, vv);
+  if (k && r.max_rows > 1) kv4_launch_write(s, dtype, cache->head_dim, p, r, kk, vv);
   if (scale == 0.f) scale = 1.0f / sqrtf((float)cache->head_dim);
-  kv4_launch_attention(s, dtype, cache->head_dim, p, r, n_heads, scale, qq, oo);
+  kv4_launch_attention(s, dtype, cache->head_dim, p, r, n_heads, scale, qq, k ? &kk : nullptr, k ? &vv : nullptr, oo, a,
+                       static_cast<float*>(workspace));
   HIPCHK(hipGetLastError());
   return LL_OK;
 }

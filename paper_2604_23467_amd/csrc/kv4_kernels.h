@@ -246,60 +246,469 @@ __global__ __launch_bounds__(256) void kv4_read_kernel(Kv4Pool p, Kv4Rows r, Kv4
   kv4_store8(which ? v : k, s.first + j, head, oct * 8, out);
 }
 
-// Attention of one row and head per wave: HD / 8 lanes hold a row of the cache, the wave's lane groups take every 64 / (HD / 8)-th
-// key, each with a running maximum and sum.  grid = (rows, ceil(heads / 4)).
+// ---- attention ----
+//
+// Scores and outputs of up to 16 query rows (rows of a sequence times the heads that share a key head) run on the matrix
+// instructions, also where there is one row only: a code costs the vector unit 1.6 operations on its way into an operand and
+// nothing more, where a product of its own would cost two.
+//
+//   S^T [32 keys][16 queries]   = K Q^T:    16x16x32 products, keys as rows, queries as columns
+//   O^T [head_dim][16 queries] += V^T P^T:  the values' elements as rows
+//
+// Both contract over an order of their own choosing, so every operand is built in the registers of the lane that loaded it,
+// without LDS.  With lane = 16 h + c:
+//  * K: the lane loads a quarter (HD / 4 elements) of key c; product s takes its 8 elements 8 s .. of all four quarters.
+//    q is laid out to match.  The middles enter by a product of their own: the lane's mid against the sum of q over the
+//    quarter, which is split into three binary16 numbers.
+//  * S^T leaves the lane with keys 4 h + i and 16 + 4 h + i (i < 4) of query c: exactly the 8 keys that the lane feeds to
+//    the second product as P^T.
+//  * V: for these 8 keys the lane loads elements (HD / 16) c ..; a permutation of half words pairs two keys, and every
+//    nibble position e is then the operand of the HD / 16 elements' e-th row block: row c of product e is element
+//    (HD / 16) c + e.  A further product's rows are the middles of the groups (row 4 g'), ones (row 1: the sum of the
+//    weights) and where a group is NaN (rows 4 g' + 2); a lane's outputs then all belong to one group, whose sum is in its
+//    own registers.
+// s (c - 8) is exact in binary16 (see above).  Weights are at most 2^15 (the maximum is taken off in front of the exponential)
+// and enter as two binary16 numbers, so that they count with 22 bits; sums are 32 bits wide.
+
+typedef half_t h2 __attribute__((ext_vector_type(2)));
+
+#define KV4_WAVES 4              // of a workgroup; they take every fourth tile
+#define KV4_TILE 32              // keys of a tile
+#define KV4_FEW_ROWS 16
+#define KV4_SHIFT 15.0f          // log2 of the largest weight
+
+__device__ __forceinline__ h2 kv4_h2(u32 v) { return __builtin_bit_cast(h2, v); }
+__device__ __forceinline__ u32 kv4_u32(h2 v) { return __builtin_bit_cast(u32, v); }
+__device__ __forceinline__ u32 kv4_lo16(u32 a, u32 b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
+__device__ __forceinline__ u32 kv4_hi16(u32 a, u32 b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
+
+// Nibbles 0 and 4, 1 and 5, 2 and 6, 3 and 7 of w as pairs of c - 8: a code set into the mantissa of 1024 (or, four bits
+// higher, of 64) is that number plus c.
+__device__ __forceinline__ void kv4_unpack(u32 w, h2 (&d)[4]) {
+  const u32 y = w >> 8;
+  d[0] = kv4_h2((w & 0x000f000fu) | 0x64006400u) - h2{1032, 1032};
+  d[1] = kv4_h2((w & 0x00f000f0u) | 0x54005400u) - h2{72, 72};
+  d[2] = kv4_h2((y & 0x000f000fu) | 0x64006400u) - h2{1032, 1032};
+  d[3] = kv4_h2((y & 0x00f000f0u) | 0x54005400u) - h2{72, 72};
+}
+
+__device__ __forceinline__ float kv4_max_over_quarters(float v) {      // lanes c, c + 16, c + 32, c + 48
+  const u32 b = __builtin_bit_cast(u32, v);
+  const auto r = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+  const float a = fmaxf(__builtin_bit_cast(float, (u32)r[0]), __builtin_bit_cast(float, (u32)r[1]));
+  const u32 d = __builtin_bit_cast(u32, a);
+  const auto t = __builtin_amdgcn_permlane16_swap(d, d, false, false);
+  return fmaxf(__builtin_bit_cast(float, (u32)t[0]), __builtin_bit_cast(float, (u32)t[1]));
+}
+
+__device__ __forceinline__ f4 kv4_mfma(h8 a, h8 b, f4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+
+// What a workgroup works on: row block rb of key head `head` of sequence b, and a share of its keys
+struct Kv4Work {
+  int b, rb, head, split;
+};
+__device__ __forceinline__ Kv4Work kv4_work(int id, int splits, int kv_heads, int row_blocks) {
+  Kv4Work w;
+  w.split = id % splits;
+  id /= splits;
+  w.head = id % kv_heads;
+  id /= kv_heads;
+  w.rb = id % row_blocks;
+  w.b = id / row_blocks;
+  return w;
+}
+// Tiles of a share when `tiles` of them are dealt to `splits` workgroups: whole rounds of the waves
+__device__ __forceinline__ int kv4_share(int tiles, int splits) {
+  return ((tiles + splits - 1) / splits + KV4_WAVES - 1) / KV4_WAVES * KV4_WAVES;
+}
+
+// Queries of a row block as the second operand, in K's order: lane (h, c) has quarter h of query c's row, scaled by a power of
+// two to a largest element of 1 .. 2 (bfloat16's 8 bits then fit binary16, whatever their exponent); and what scores have to be
+// multiplied by for a softmax to the base 2.
+template <int HD>
+struct Kv4Query {
+  h8 q[HD / 32];
+  h8 sums;
+  float scale;
+};
 template <class T, int HD>
-__global__ __launch_bounds__(256) void kv4_attn_simple_kernel(Kv4Pool p, Kv4Rows r, Kv4View q, Kv4View o, int heads,
-                                                              float scale) {
-  constexpr int LPR = HD / 8, GPW = 64 / LPR;
-  const int b = kv4_find(r, blockIdx.x);
-  const int lane = threadIdx.x & 63, h = blockIdx.y * 4 + (threadIdx.x >> 6);
-  const int gi = lane / LPR, li = lane % LPR;
-  if (h >= heads || b < 0) return;
-  const Kv4Seq s = kv4_seq(r, b);
-  const int j = blockIdx.x - s.first;
-  if (j >= r.max_rows) return;
-  const int kh = h / (heads / p.kv_heads), n_keys = s.len - s.rows + j + 1;
-  const int* table = r.table + (size_t)b * r.table_stride;
-  const u16x8 qin = kv4_load8(q, s.first + j, h, li * 8);
-  float qv[8], acc[8], m = -INFINITY, l = 0.f;
+__device__ __forceinline__ void kv4_load_query(const Kv4View& v, bool there, int row, int head, int h, float scale, Kv4Query<HD>& out) {
+  float x[HD / 32][8], top = 0.f;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) { qv[e] = T::load(qin[e]) * scale; acc[e] = 0.f; }
-  for (int u = gi; u < n_keys; u += GPW) {
-    const int row = kv4_row(p, table, r.table_stride, u);
-    if (row < 0) continue;
-    const u32 kw = *(const u32*)(kv4_codes<HD>(p, 0, kh) + (size_t)row * (HD / 2) + li * 4);
-    const u32 vw = *(const u32*)(kv4_codes<HD>(p, 1, kh) + (size_t)row * (HD / 2) + li * 4);
-    const u32 kp = *(const u32*)(kv4_params<HD>(p, 0, kh) + (size_t)row * (HD / 8) + li / 4 * 4);
-    const u32 vp = *(const u32*)(kv4_params<HD>(p, 1, kh) + (size_t)row * (HD / 8) + li / 4 * 4);
-    float dot = 0.f;
+  for (int s = 0; s < HD / 32; ++s) {
+    u16x8 in{};
+    if (there) in = kv4_load8(v, row, head, h * (HD / 4) + s * 8);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) dot += qv[e] * kv4_value(kw, e, Kv4F16::load(kp & 0xffff), Kv4F16::load(kp >> 16));
-    dot = group_sum<LPR>(dot);
-    const float mn = fmaxf(m, dot), corr = m == mn ? 1.f : __expf(m - mn), pr = __expf(dot - mn);
-    l = l * corr + pr;
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-      acc[e] = acc[e] * corr + pr * kv4_value(vw, e, Kv4F16::load(vp & 0xffff), Kv4F16::load(vp >> 16));
-    m = mn;
+    for (int i = 0; i < 8; ++i) {
+      x[s][i] = T::load(in[i]);
+      top = fmaxf(top, fabsf(x[s][i]));
+    }
   }
-  float M = m;
+  top = kv4_max_over_quarters(top);
+  int e = 0;
+  if (top > 0.f && top < INFINITY) e = ilogbf(top);
+  float sum = 0.f;
 #pragma unroll
-  for (int off = LPR; off < 64; off <<= 1) M = fmaxf(M, __shfl_xor(M, off));
-  const float w = M > -INFINITY ? __expf(m - M) : 0.f;
-  l *= w;
+  for (int s = 0; s < HD / 32; ++s) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e) acc[e] *= w;
-#pragma unroll
-  for (int off = LPR; off < 64; off <<= 1) {
-    l += __shfl_xor(l, off);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) acc[e] += __shfl_xor(acc[e], off);
+    for (int i = 0; i < 4; ++i) {          // pairs (i, i + 4), as a word of codes unpacks
+      const half_t a = (half_t)ldexpf(x[s][i], -e), b = (half_t)ldexpf(x[s][i + 4], -e);
+      out.q[s][2 * i] = a;
+      out.q[s][2 * i + 1] = b;
+      sum += (float)a + (float)b;
+    }
   }
-  if (gi == 0) {
-    u16x8 out;
+  const half_t s1 = (half_t)sum, s2 = (half_t)(sum - (float)s1), s3 = (half_t)(sum - (float)s1 - (float)s2);
+  out.sums = h8{s1, s2, s3, 0, 0, 0, 0, 0};
+  out.scale = ldexpf(scale * 1.44269504088896340736f, e);
+}
+
+// A tile of 32 keys as it lies in the pool: the lane's part of keys c and 16 + c and of its 8 values
+template <int HD>
+struct Kv4Tile {
+  u32 k[2][HD / 32], kp[2], v[8], vp[8];
+  int row[8];                   // pool rows of the lane's 8 values, -1: not there
+};
+
+template <int HD>
+struct Kv4Keys {
+  const char *kc, *kp, *vc, *vp;      // codes and parameters of the key head, moved to the lane's part of a row
+  __device__ __forceinline__ Kv4Keys(const Kv4Pool& p, int head, int h, int c) {
+    kc = kv4_codes<HD>(p, 0, head) + h * (HD / 8);
+    kp = kv4_params<HD>(p, 0, head) + (HD == 128 ? h : h >> 1) * 4;
+    vc = kv4_codes<HD>(p, 1, head) + c * (HD / 32);
+    vp = kv4_params<HD>(p, 1, head) + (c * (HD / 16) / KV4_GROUP) * 4;
+  }
+  // rows: the tile's 32 pool rows in LDS
+  __device__ __forceinline__ void load(const int* rows, int h, int c, Kv4Tile<HD>& t) const {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) out[e] = T::store(l != 0.f ? acc[e] / l : 0.f);
-    kv4_store8(o, s.first + j, h, li * 8, out);
+    for (int j = 0; j < 2; ++j) {
+      const u32 r = max(rows[16 * j + c], 0);
+      const char* a = kc + (size_t)(r * (u32)(HD / 2));
+      if (HD == 128) {
+        const u32x4 w = *as_global(reinterpret_cast<const u32x4*>(a));
+#pragma unroll
+        for (int s = 0; s < HD / 32; ++s) t.k[j][s] = w[s];
+      } else {
+        const u32x2 w = *as_global(reinterpret_cast<const u32x2*>(a));
+#pragma unroll
+        for (int s = 0; s < HD / 32; ++s) t.k[j][s] = w[s];
+      }
+      t.kp[j] = *as_global(reinterpret_cast<const u32*>(kp + (size_t)(r * (u32)(HD / 8))));
+    }
+    const int4 a = *reinterpret_cast<const int4*>(rows + 4 * h), b = *reinterpret_cast<const int4*>(rows + 16 + 4 * h);
+    t.row[0] = a.x; t.row[1] = a.y; t.row[2] = a.z; t.row[3] = a.w;
+    t.row[4] = b.x; t.row[5] = b.y; t.row[6] = b.z; t.row[7] = b.w;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const u32 r = max(t.row[j], 0);
+      if (HD == 128) t.v[j] = *as_global(reinterpret_cast<const u32*>(vc + (size_t)(r * (u32)(HD / 2))));
+      else t.v[j] = *as_global(reinterpret_cast<const u16*>(vc + (size_t)(r * (u32)(HD / 2))));
+      t.vp[j] = *as_global(reinterpret_cast<const u32*>(vp + (size_t)(r * (u32)(HD / 8))));
+    }
+  }
+};
+
+// Keys of a tile against the queries: S^T of keys 16 j + 4 h + i
+template <int HD>
+__device__ __forceinline__ void kv4_scores(const Kv4Tile<HD>& t, const Kv4Query<HD>& q, f4 (&s)[2]) {
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const half_t mid = kv4_h2(t.kp[j])[1];
+    s[j] = kv4_mfma(h8{mid, mid, mid, 0, 0, 0, 0, 0}, q.sums, f4{0.f, 0.f, 0.f, 0.f});
+    const h2 step = kv4_h2(kv4_lo16(t.kp[j], t.kp[j]));
+#pragma unroll
+    for (int n = 0; n < HD / 32; ++n) {
+      h2 d[4];
+      kv4_unpack(t.k[j][n], d);
+      u32x4 a;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) a[i] = kv4_u32(d[i] * step);
+      s[j] = kv4_mfma(__builtin_bit_cast(h8, a), q.q[n], s[j]);
+    }
+  }
+}
+
+// Values of a tile as operands: o[e] is row block e (element (HD / 16) c + e of the lane's 8 keys), o[HD / 16] the block
+// of middles, ones and NaN marks
+template <int HD>
+__device__ __forceinline__ void kv4_value_operands(Kv4Tile<HD>& t, int c, h8 (&o)[HD / 16 + 1]) {
+  // Keys that are not there, and groups that are NaN, must not meet a weight of zero.  Both are rare and found for the whole
+  // wave at once: a sum of all middles is NaN if one is.
+  u32 marks = 0;
+  int low = t.row[0];
+  h2 all = kv4_h2(t.vp[0]);
+#pragma unroll
+  for (int j = 1; j < 8; ++j) {
+    low = min(low, t.row[j]);
+    all += kv4_h2(t.vp[j]);
+  }
+  if (__any(low < 0 || !(all[1] == all[1]))) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const half_t mid = kv4_h2(t.vp[j])[1];
+      if (t.row[j] < 0) t.vp[j] = 0;
+      else if (!(mid == mid)) { t.vp[j] = 0; marks |= 1u << j; }
+    }
+  }
+  u32x4 w[HD / 16 + 1];
+#pragma unroll
+  for (int a = 0; a < 4; ++a) {
+    const h2 step = kv4_h2(kv4_lo16(t.vp[2 * a], t.vp[2 * a + 1]));
+    w[HD / 16][a] = kv4_hi16(t.vp[2 * a], t.vp[2 * a + 1]);
+    h2 d[4];
+    kv4_unpack(kv4_lo16(t.v[2 * a], t.v[2 * a + 1]), d);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i][a] = kv4_u32(d[i] * step);
+    if (HD == 128) {
+      kv4_unpack(kv4_hi16(t.v[2 * a], t.v[2 * a + 1]), d);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[4 * (HD / 128) + i][a] = kv4_u32(d[i] * step);
+    }
+  }
+  if ((c & 3) == 2) {
+#pragma unroll
+    for (int a = 0; a < 4; ++a)
+      w[HD / 16][a] = ((marks >> (2 * a)) & 1 ? 0x3c00u : 0u) | ((marks >> (2 * a + 1)) & 1 ? 0x3c000000u : 0u);
+  } else if (c & 3) {
+    const u32 one = c == 1 ? 0x3c003c00u : 0u;
+    w[HD / 16] = u32x4{one, one, one, one};
+  }
+#pragma unroll
+  for (int e = 0; e <= HD / 16; ++e) o[e] = __builtin_bit_cast(h8, w[e]);
+}
+
+// Up to 16 query rows of one key head.  grid = splits * kv_heads * row blocks * sequences workgroups (kv4_work's order) of four
+// waves; the waves take every fourth tile of the workgroup's share and keep a softmax of their own, which meet in LDS.
+// NEW: knew and vnew hold the sequences' last rows (one row each), which the workgroup that has the last key quantises into
+// the pool and attends from LDS.  part: with more than one split, the shares' results ([work][16][HD + 2] floats).
+template <class T, int HD, bool NEW>
+__global__ __launch_bounds__(256) void kv4_attn_few_kernel(Kv4Pool p, Kv4Rows r, Kv4View q, Kv4View o, Kv4View knew, Kv4View vnew,
+                                                           int heads, float scale, int splits, int row_blocks, float* part) {
+  constexpr int NE = HD / 16;
+  struct Meet { float acc[KV4_WAVES][NE + 1][64][4]; };
+  __shared__ union {
+    Meet meet;
+    float out[16][HD + 4];
+  } s_mem;
+  __shared__ int s_rows[KV4_WAVES][2][KV4_TILE];
+  __shared__ float s_m[KV4_WAVES][16];
+  __shared__ u32 s_new[2][HD / 8], s_newp[2][HD / 32];
+  const Kv4Work w = kv4_work(blockIdx.x, splits, p.kv_heads, row_blocks);
+  const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, h = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const Kv4Seq s = kv4_seq(r, w.b);
+  const int share_heads = heads / p.kv_heads, rows = min(s.rows, r.max_rows) * share_heads;
+  const int f0 = w.rb * KV4_FEW_ROWS;
+  if (f0 >= rows) return;
+  const int f = f0 + c, j = f / share_heads, qhead = w.head * share_heads + f - j * share_heads;
+  const bool there = f < rows;
+  const int limit = there ? s.len - s.rows + j : -1;                       // last position that the lane's query sees
+  const int first_limit = s.len - s.rows + f0 / share_heads;
+  const int n_keys = max(s.len - s.rows + min(f0 + KV4_FEW_ROWS - 1, rows - 1) / share_heads + 1, 0);
+  const int tiles = (n_keys + KV4_TILE - 1) / KV4_TILE, share = kv4_share(tiles, splits);
+  const int t0 = w.split * share, t1 = min(t0 + share, tiles);
+  if (w.split > 0 && t0 >= tiles) return;
+  const int* table = r.table + (size_t)w.b * r.table_stride;
+
+  const Kv4Keys<HD> keys(p, w.head, h, c);
+  auto look = [&](int t, int buf) {                                        // pool rows of tile t
+    const int u = t * KV4_TILE + (lane & 31);
+    s_rows[wave][buf][lane & 31] = u < n_keys ? kv4_row(p, table, r.table_stride, u) : -1;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  };
+
+  Kv4Query<HD> query;
+  kv4_load_query<T, HD>(q, there, s.first + j, qhead, h, scale, query);
+  const int pnew = NEW ? s.len - s.rows : -1;
+  if (NEW && pnew >= 0 && pnew / KV4_TILE >= t0 && pnew / KV4_TILE < t1) {
+    if (wave < 2 && lane < HD / 8) {
+      const u16x8 in = kv4_load8(wave ? vnew : knew, s.first, w.head, lane * 8);
+      float x[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = T::load(in[i]);
+      u32 param;
+      const u32 code = kv4_quantise(x, param);
+      s_new[wave][lane] = code;
+      s_newp[wave][lane >> 2] = param;
+      const int row = kv4_row(p, table, r.table_stride, pnew);
+      if (row >= 0) {
+        *(u32*)(kv4_codes<HD>(p, wave, w.head) + (size_t)row * (HD / 2) + lane * 4) = code;
+        if (lane % 4 == 0) *(u32*)(kv4_params<HD>(p, wave, w.head) + (size_t)row * (HD / 8) + lane) = param;
+      }
+    }
+    __syncthreads();
+  }
+
+  f4 acc[NE + 1];
+#pragma unroll
+  for (int e = 0; e <= NE; ++e) acc[e] = f4{0.f, 0.f, 0.f, 0.f};
+  float m = -INFINITY;
+
+  auto use = [&](int t, Kv4Tile<HD>& tile) {
+    const int u0 = t * KV4_TILE;
+    if (NEW && pnew >= u0 && pnew < u0 + KV4_TILE) {
+      const int at = pnew - u0;
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+        if (at == 16 * n + c) {
+#pragma unroll
+          for (int i = 0; i < HD / 32; ++i) tile.k[n][i] = s_new[0][h * (HD / 32) + i];
+          tile.kp[n] = s_newp[0][HD == 128 ? h : h >> 1];
+        }
+#pragma unroll
+      for (int n = 0; n < 8; ++n)
+        if (at == (n & 3) + 4 * h + 16 * (n >> 2)) {
+          tile.v[n] = HD == 128 ? s_new[1][c] : (s_new[1][c >> 1] >> (16 * (c & 1))) & 0xffff;
+          tile.vp[n] = s_newp[1][c * (HD / 16) / KV4_GROUP];
+        }
+    }
+    f4 sc[2];
+    kv4_scores<HD>(tile, query, sc);
+    float x[8], top = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = sc[i >> 2][i & 3] * query.scale;
+    int low = tile.row[0];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) low = min(low, tile.row[i]);
+    if (u0 + KV4_TILE - 1 > first_limit || __any(low < 0)) {               // some query does not see some key
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (tile.row[i] < 0 || u0 + (i & 3) + 4 * h + 16 * (i >> 2) > limit) x[i] = -INFINITY;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = fmaxf(top, x[i]);
+    top = fmaxf(kv4_max_over_quarters(top), m);
+    if (__any(top > m)) {
+      const float corr = top > m ? __builtin_amdgcn_exp2f(m - top) : 1.0f;
+      m = top;
+#pragma unroll
+      for (int e = 0; e <= NE; ++e) acc[e] *= corr;
+    }
+    const float base = (m > -INFINITY ? m : 0.f) - KV4_SHIFT;
+    h8 ph, pl;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float v = __builtin_amdgcn_exp2f(x[i] - base);
+      ph[i] = (half_t)v;
+      pl[i] = (half_t)(v - (float)ph[i]);
+    }
+    h8 op[NE + 1];
+    kv4_value_operands<HD>(tile, c, op);
+#pragma unroll
+    for (int e = 0; e <= NE; ++e) {
+      acc[e] = kv4_mfma(op[e], ph, acc[e]);
+      acc[e] = kv4_mfma(op[e], pl, acc[e]);
+    }
+  };
+
+  Kv4Tile<HD> a, b;
+  int t = t0 + wave;
+  if (t < t1) {
+    look(t, 0);
+    keys.load(s_rows[wave][0], h, c, a);
+  }
+  for (; t < t1; t += 2 * KV4_WAVES) {
+    if (t + KV4_WAVES < t1) {
+      look(t + KV4_WAVES, 1);
+      keys.load(s_rows[wave][1], h, c, b);
+    }
+    use(t, a);
+    if (t + KV4_WAVES >= t1) break;
+    if (t + 2 * KV4_WAVES < t1) {
+      look(t + 2 * KV4_WAVES, 0);
+      keys.load(s_rows[wave][0], h, c, a);
+    }
+    use(t + KV4_WAVES, b);
+  }
+
+  // the waves' softmaxes meet
+  if (h == 0) s_m[wave][c] = m;
+  __syncthreads();
+  float top = s_m[0][c];
+#pragma unroll
+  for (int i = 1; i < KV4_WAVES; ++i) top = fmaxf(top, s_m[i][c]);
+  const float weight = m > -INFINITY ? __builtin_amdgcn_exp2f(m - top) : 0.f;
+#pragma unroll
+  for (int e = 0; e <= NE; ++e)
+    *reinterpret_cast<f4*>(s_mem.meet.acc[wave][e][lane]) = acc[e] * weight;
+  __syncthreads();
+  f4 sums[NE / KV4_WAVES], extra{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int n = 0; n < NE / KV4_WAVES; ++n) {
+    sums[n] = f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < KV4_WAVES; ++i) sums[n] += *reinterpret_cast<const f4*>(s_mem.meet.acc[i][wave * (NE / KV4_WAVES) + n][lane]);
+  }
+#pragma unroll
+  for (int i = 0; i < KV4_WAVES; ++i) extra += *reinterpret_cast<const f4*>(s_mem.meet.acc[i][NE][lane]);
+  float l = 0.f;
+#pragma unroll
+  for (int i = 0; i < KV4_WAVES; ++i) l += s_mem.meet.acc[i][NE][c][1];
+  __syncthreads();
+  const float mid = extra[2] != 0.f ? NAN : extra[0];                      // a NaN mark with any weight
+  const float inv = splits > 1 ? 1.0f : l != 0.f ? 1.0f / l : 0.f;
+#pragma unroll
+  for (int n = 0; n < NE / KV4_WAVES; ++n)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {                                          // element (HD / 16) (4 h + i) + e
+      const int e = (HD / 16) * (4 * h + i) + wave * (NE / KV4_WAVES) + n;
+      s_mem.out[c][e] = (sums[n][i] + mid) * inv;
+    }
+  __syncthreads();
+  if (splits == 1) {
+    for (int i = tid; i < 16 * (HD / 8); i += 256) {
+      const int row = i / (HD / 8), oct = i % (HD / 8), ff = f0 + row, jj = ff / share_heads;
+      if (ff >= rows) break;
+      u16x8 v;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = T::store(s_mem.out[row][oct * 8 + e]);
+      kv4_store8(o, s.first + jj, w.head * share_heads + ff - jj * share_heads, oct * 8, v);
+    }
+  } else {
+    float* to = part + (size_t)blockIdx.x * 16 * (HD + 2);
+    for (int i = tid; i < min(16, rows - f0) * (HD / 4); i += 256) {
+      const int row = i / (HD / 4), x = i % (HD / 4);
+      *reinterpret_cast<f4*>(to + row * HD + x * 4) = *reinterpret_cast<const f4*>(&s_mem.out[row][x * 4]);
+    }
+    if (tid < 16) {
+      to[16 * HD + tid] = top;
+      to[16 * HD + 16 + tid] = l;
+    }
+  }
+}
+
+// The shares of a row block together: grid = kv_heads * row blocks * sequences
+template <class T, int HD>
+__global__ __launch_bounds__(256) void kv4_join_kernel(Kv4Pool p, Kv4Rows r, Kv4View o, int heads, int splits, int row_blocks,
+                                                       const float* part) {
+  const Kv4Work w = kv4_work(blockIdx.x, 1, p.kv_heads, row_blocks);
+  const Kv4Seq s = kv4_seq(r, w.b);
+  const int share_heads = heads / p.kv_heads, rows = min(s.rows, r.max_rows) * share_heads;
+  const int f0 = w.rb * KV4_FEW_ROWS;
+  if (f0 >= rows) return;
+  const int n_keys = max(s.len - s.rows + min(f0 + KV4_FEW_ROWS - 1, rows - 1) / share_heads + 1, 0);
+  const int tiles = (n_keys + KV4_TILE - 1) / KV4_TILE, share = kv4_share(tiles, splits);
+  const int n = tiles ? (tiles + share - 1) / share : 1;
+  const float* from = part + (size_t)blockIdx.x * splits * 16 * (HD + 2);
+  for (int i = threadIdx.x; i < min(16, rows - f0) * (HD / 8); i += 256) {
+    const int row = i / (HD / 8), oct = i % (HD / 8), ff = f0 + row, jj = ff / share_heads;
+    float top = -INFINITY;
+    for (int k = 0; k < n; ++k) top = fmaxf(top, from[(size_t)k * 16 * (HD + 2) + 16 * HD + row]);
+    float l = 0.f;
+    f4 a{0.f, 0.f, 0.f, 0.f}, b = a;
+    for (int k = 0; k < n; ++k) {
+      const float* f = from + (size_t)k * 16 * (HD + 2);
+      const float m = f[16 * HD + row], x = m > -INFINITY ? __builtin_amdgcn_exp2f(m - top) : 0.f;
+      l += x * f[16 * HD + 16 + row];
+      a += x * *reinterpret_cast<const f4*>(f + row * HD + oct * 8);
+      b += x * *reinterpret_cast<const f4*>(f + row * HD + oct * 8 + 4);
+    }
+    const float inv = l != 0.f ? 1.0f / l : 0.f;
+    u16x8 v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) { v[e] = T::store(a[e] * inv); v[4 + e] = T::store(b[e] * inv); }
+    kv4_store8(o, s.first + jj, w.head * share_heads + ff - jj * share_heads, oct * 8, v);
   }
 }
