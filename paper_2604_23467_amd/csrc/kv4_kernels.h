@@ -22,6 +22,7 @@ typedef uint16_t u16;
 typedef uint32_t u32;
 typedef u32 u32x2 __attribute__((ext_vector_type(2)));
 typedef u32 u32x4 __attribute__((ext_vector_type(4)));
+typedef u32 u32x8 __attribute__((ext_vector_type(8)));
 typedef u16 u16x8 __attribute__((ext_vector_type(8)));
 
 // One layer's pool
@@ -363,92 +364,94 @@ __device__ __forceinline__ void kv4_load_query(const Kv4View& v, bool there, int
   out.scale = ldexpf(scale * 1.44269504088896340736f, e);
 }
 
-// A tile of 32 keys as it lies in the pool: the lane's part of keys c and 16 + c and of its 8 values
+// A tile of 32 keys as it lies in the pool: the lane's part of keys c and 16 + c, and of its 8 values
 template <int HD>
 struct Kv4Tile {
-  u32 k[2][HD / 32], kp[2], v[8], vp[8];
-  int row[8];                   // pool rows of the lane's 8 values, -1: not there
+  u32x4 k0, k1;                 // (head_dim 64: the first two words)
+  u32x2 kp;
+  u32x8 v, vp;
 };
 
 template <int HD>
 struct Kv4Keys {
-  const char *kc, *kp, *vc, *vp;      // codes and parameters of the key head, moved to the lane's part of a row
+  const char *kc, *kp, *vc, *vp;      // codes and parameters of the key head
+  u32 kc_at, kp_at, vc_at, vp_at;     // the lane's part of a row
   __device__ __forceinline__ Kv4Keys(const Kv4Pool& p, int head, int h, int c) {
-    kc = kv4_codes<HD>(p, 0, head) + h * (HD / 8);
-    kp = kv4_params<HD>(p, 0, head) + (HD == 128 ? h : h >> 1) * 4;
-    vc = kv4_codes<HD>(p, 1, head) + c * (HD / 32);
-    vp = kv4_params<HD>(p, 1, head) + (c * (HD / 16) / KV4_GROUP) * 4;
+    kc = kv4_codes<HD>(p, 0, head);
+    kp = kv4_params<HD>(p, 0, head);
+    vc = kv4_codes<HD>(p, 1, head);
+    vp = kv4_params<HD>(p, 1, head);
+    kc_at = h * (HD / 8);
+    kp_at = (HD == 128 ? h : h >> 1) * 4;
+    vc_at = c * (HD / 32);
+    vp_at = (c * (HD / 16) / KV4_GROUP) * 4;
+  }
+  template <class W>
+  static __device__ __forceinline__ W get(const char* base, u32 row, u32 bytes, u32 at) {
+    return *as_global(reinterpret_cast<const W*>(base + (size_t)(row * bytes + at)));
   }
   // rows: the tile's 32 pool rows in LDS
-  __device__ __forceinline__ void load(const int* rows, int h, int c, Kv4Tile<HD>& t) const {
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const u32 r = max(rows[16 * j + c], 0);
-      const char* a = kc + (size_t)(r * (u32)(HD / 2));
-      if (HD == 128) {
-        const u32x4 w = *as_global(reinterpret_cast<const u32x4*>(a));
-#pragma unroll
-        for (int s = 0; s < HD / 32; ++s) t.k[j][s] = w[s];
-      } else {
-        const u32x2 w = *as_global(reinterpret_cast<const u32x2*>(a));
-#pragma unroll
-        for (int s = 0; s < HD / 32; ++s) t.k[j][s] = w[s];
-      }
-      t.kp[j] = *as_global(reinterpret_cast<const u32*>(kp + (size_t)(r * (u32)(HD / 8))));
+  __device__ __forceinline__ void load(const u32* rows, int h, int c, Kv4Tile<HD>& t) const {
+    const u32 r0 = rows[c], r1 = rows[16 + c];
+    const u32x4 a = *reinterpret_cast<const u32x4*>(rows + 4 * h), b = *reinterpret_cast<const u32x4*>(rows + 16 + 4 * h);
+    if (HD == 128) {
+      t.k0 = get<u32x4>(kc, r0, HD / 2, kc_at);
+      t.k1 = get<u32x4>(kc, r1, HD / 2, kc_at);
+    } else {
+      const u32x2 x = get<u32x2>(kc, r0, HD / 2, kc_at), y = get<u32x2>(kc, r1, HD / 2, kc_at);
+      t.k0 = u32x4{x[0], x[1], 0, 0};
+      t.k1 = u32x4{y[0], y[1], 0, 0};
     }
-    const int4 a = *reinterpret_cast<const int4*>(rows + 4 * h), b = *reinterpret_cast<const int4*>(rows + 16 + 4 * h);
-    t.row[0] = a.x; t.row[1] = a.y; t.row[2] = a.z; t.row[3] = a.w;
-    t.row[4] = b.x; t.row[5] = b.y; t.row[6] = b.z; t.row[7] = b.w;
+    t.kp = u32x2{get<u32>(kp, r0, HD / 8, kp_at), get<u32>(kp, r1, HD / 8, kp_at)};
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const u32 r = max(t.row[j], 0);
-      if (HD == 128) t.v[j] = *as_global(reinterpret_cast<const u32*>(vc + (size_t)(r * (u32)(HD / 2))));
-      else t.v[j] = *as_global(reinterpret_cast<const u16*>(vc + (size_t)(r * (u32)(HD / 2))));
-      t.vp[j] = *as_global(reinterpret_cast<const u32*>(vp + (size_t)(r * (u32)(HD / 8))));
+      const u32 r = j < 4 ? a[j] : b[j - 4];
+      t.v[j] = HD == 128 ? get<u32>(vc, r, HD / 2, vc_at) : (u32)get<u16>(vc, r, HD / 2, vc_at);
+      t.vp[j] = get<u32>(vp, r, HD / 8, vp_at);
     }
   }
 };
 
 // Keys of a tile against the queries: S^T of keys 16 j + 4 h + i
 template <int HD>
-__device__ __forceinline__ void kv4_scores(const Kv4Tile<HD>& t, const Kv4Query<HD>& q, f4 (&s)[2]) {
-#pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    const half_t mid = kv4_h2(t.kp[j])[1];
-    s[j] = kv4_mfma(h8{mid, mid, mid, 0, 0, 0, 0, 0}, q.sums, f4{0.f, 0.f, 0.f, 0.f});
-    const h2 step = kv4_h2(kv4_lo16(t.kp[j], t.kp[j]));
+__device__ __forceinline__ void kv4_scores(const Kv4Tile<HD>& t, const Kv4Query<HD>& q, f4& s0, f4& s1) {
+  auto one = [&](u32x4 w, u32 param) {
+    const half_t mid = kv4_h2(param)[1];
+    f4 s = kv4_mfma(h8{mid, mid, mid, 0, 0, 0, 0, 0}, q.sums, f4{0.f, 0.f, 0.f, 0.f});
+    const h2 step = kv4_h2(kv4_lo16(param, param));
 #pragma unroll
     for (int n = 0; n < HD / 32; ++n) {
       h2 d[4];
-      kv4_unpack(t.k[j][n], d);
-      u32x4 a;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) a[i] = kv4_u32(d[i] * step);
-      s[j] = kv4_mfma(__builtin_bit_cast(h8, a), q.q[n], s[j]);
+      kv4_unpack(w[n], d);
+      const u32x4 a{kv4_u32(d[0] * step), kv4_u32(d[1] * step), kv4_u32(d[2] * step), kv4_u32(d[3] * step)};
+      s = kv4_mfma(__builtin_bit_cast(h8, a), q.q[n], s);
     }
-  }
+    return s;
+  };
+  s0 = one(t.k0, t.kp[0]);
+  s1 = one(t.k1, t.kp[1]);
 }
 
+// Bit of the lane's i-th key (keys 4 h .. and 16 + 4 h ..) in a word with a bit for each of a tile's keys
+__device__ __forceinline__ int kv4_key(int i, int h) { return (i & 3) + 4 * h + 16 * (i >> 2); }
+
 // Values of a tile as operands: o[e] is row block e (element (HD / 16) c + e of the lane's 8 keys), o[HD / 16] the block
-// of middles, ones and NaN marks
+// of middles, ones and NaN marks.  there: which of the tile's keys have a row.
 template <int HD>
-__device__ __forceinline__ void kv4_value_operands(Kv4Tile<HD>& t, int c, h8 (&o)[HD / 16 + 1]) {
+__device__ __forceinline__ void kv4_value_operands(Kv4Tile<HD>& t, u32 there, int c, int h, h8 (&o)[HD / 16 + 1]) {
   // Keys that are not there, and groups that are NaN, must not meet a weight of zero.  Both are rare and found for the whole
   // wave at once: a sum of all middles is NaN if one is.
   u32 marks = 0;
-  int low = t.row[0];
   h2 all = kv4_h2(t.vp[0]);
 #pragma unroll
-  for (int j = 1; j < 8; ++j) {
-    low = min(low, t.row[j]);
-    all += kv4_h2(t.vp[j]);
-  }
-  if (__any(low < 0 || !(all[1] == all[1]))) {
+  for (int j = 1; j < 8; ++j) all += kv4_h2(t.vp[j]);
+  if (~there || __any(!(all[1] == all[1]))) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const half_t mid = kv4_h2(t.vp[j])[1];
-      if (t.row[j] < 0) t.vp[j] = 0;
-      else if (!(mid == mid)) { t.vp[j] = 0; marks |= 1u << j; }
+      const bool gone = !(there >> kv4_key(j, h) & 1), nan = !(mid == mid);
+      if (nan && !gone) marks |= 1u << j;
+      if (gone || nan) t.vp[j] = 0;
     }
   }
   u32x4 w[HD / 16 + 1];
@@ -466,13 +469,13 @@ __device__ __forceinline__ void kv4_value_operands(Kv4Tile<HD>& t, int c, h8 (&o
       for (int i = 0; i < 4; ++i) w[4 * (HD / 128) + i][a] = kv4_u32(d[i] * step);
     }
   }
-  if ((c & 3) == 2) {
+  const u32 fill = c == 1 ? 0x3c003c00u : 0u;
+#pragma unroll
+  for (int a = 0; a < 4; ++a) w[HD / 16][a] = (c & 3) == 0 ? w[HD / 16][a] : fill;
+  if (marks && (c & 3) == 2) {
 #pragma unroll
     for (int a = 0; a < 4; ++a)
-      w[HD / 16][a] = ((marks >> (2 * a)) & 1 ? 0x3c00u : 0u) | ((marks >> (2 * a + 1)) & 1 ? 0x3c000000u : 0u);
-  } else if (c & 3) {
-    const u32 one = c == 1 ? 0x3c003c00u : 0u;
-    w[HD / 16] = u32x4{one, one, one, one};
+      w[HD / 16][a] = (marks >> (2 * a) & 1 ? 0x3c00u : 0u) | (marks >> (2 * a + 1) & 1 ? 0x3c000000u : 0u);
   }
 #pragma unroll
   for (int e = 0; e <= HD / 16; ++e) o[e] = __builtin_bit_cast(h8, w[e]);
@@ -483,7 +486,7 @@ __device__ __forceinline__ void kv4_value_operands(Kv4Tile<HD>& t, int c, h8 (&o
 // NEW: knew and vnew hold the sequences' last rows (one row each), which the workgroup that has the last key quantises into
 // the pool and attends from LDS.  part: with more than one split, the shares' results ([work][16][HD + 2] floats).
 template <class T, int HD, bool NEW>
-__global__ __launch_bounds__(256) void kv4_attn_few_kernel(Kv4Pool p, Kv4Rows r, Kv4View q, Kv4View o, Kv4View knew, Kv4View vnew,
+__global__ __launch_bounds__(256, 2) void kv4_attn_few_kernel(Kv4Pool p, Kv4Rows r, Kv4View q, Kv4View o, Kv4View knew, Kv4View vnew,
                                                            int heads, float scale, int splits, int row_blocks, float* part) {
   constexpr int NE = HD / 16;
   struct Meet { float acc[KV4_WAVES][NE + 1][64][4]; };
@@ -491,9 +494,9 @@ __global__ __launch_bounds__(256) void kv4_attn_few_kernel(Kv4Pool p, Kv4Rows r,
     Meet meet;
     float out[16][HD + 4];
   } s_mem;
-  __shared__ int s_rows[KV4_WAVES][2][KV4_TILE];
+  __shared__ __attribute__((aligned(16))) u32 s_rows[KV4_WAVES][2][KV4_TILE];
   __shared__ float s_m[KV4_WAVES][16];
-  __shared__ u32 s_new[2][HD / 8], s_newp[2][HD / 32];
+  __shared__ __attribute__((aligned(16))) u32 s_new[2][HD / 8], s_newp[2][HD / 32];
   const Kv4Work w = kv4_work(blockIdx.x, splits, p.kv_heads, row_blocks);
   const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, h = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -512,11 +515,18 @@ __global__ __launch_bounds__(256) void kv4_attn_few_kernel(Kv4Pool p, Kv4Rows r,
   const int* table = r.table + (size_t)w.b * r.table_stride;
 
   const Kv4Keys<HD> keys(p, w.head, h, c);
-  auto look = [&](int t, int buf) {                                        // pool rows of tile t
-    const int u = t * KV4_TILE + (lane & 31);
-    s_rows[wave][buf][lane & 31] = u < n_keys ? kv4_row(p, table, r.table_stride, u) : -1;
+  // Pool rows of a tile: the page table's entries are requested a tile ahead of the tile's own loads, so that the wait for them
+  // leaves those in flight; row() then leaves the rows in LDS (0 where there is none) and returns which keys have one.
+  const int ahead = lane & (KV4_TILE - 1);
+  auto page = [&](int t) { return (int)(__umulhi((u32)(t * KV4_TILE + ahead) << 1, p.magic) >> p.shift); };
+  auto look = [&](int t) { return *as_global(table + min(page(t), r.table_stride - 1)); };
+  auto row = [&](int t, int at, int buf) {
+    const int u = t * KV4_TILE + ahead, pg = page(t);
+    const bool ok = u < n_keys && pg < r.table_stride && (u32)at <= (u32)(p.pool_rows - p.page_tokens);
+    s_rows[wave][buf][ahead] = ok ? at + (u - pg * p.page_tokens) : 0;
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
+    return (u32)__ballot(ok);
   };
 
   Kv4Query<HD> query;
@@ -546,39 +556,34 @@ __global__ __launch_bounds__(256) void kv4_attn_few_kernel(Kv4Pool p, Kv4Rows r,
   for (int e = 0; e <= NE; ++e) acc[e] = f4{0.f, 0.f, 0.f, 0.f};
   float m = -INFINITY;
 
-  auto use = [&](int t, Kv4Tile<HD>& tile) {
+  auto use = [&](int t, Kv4Tile<HD>& tile, u32 there_mask) {
     const int u0 = t * KV4_TILE;
     if (NEW && pnew >= u0 && pnew < u0 + KV4_TILE) {
       const int at = pnew - u0;
-#pragma unroll
-      for (int n = 0; n < 2; ++n)
-        if (at == 16 * n + c) {
-#pragma unroll
-          for (int i = 0; i < HD / 32; ++i) tile.k[n][i] = s_new[0][h * (HD / 32) + i];
-          tile.kp[n] = s_newp[0][HD == 128 ? h : h >> 1];
-        }
+      const u32x4 code = HD == 128 ? *reinterpret_cast<const u32x4*>(&s_new[0][h * (HD / 32)])
+                                   : u32x4{s_new[0][2 * h], s_new[0][2 * h + 1], 0, 0};
+      const u32 param = s_newp[0][HD == 128 ? h : h >> 1];
+      if (at == c) { tile.k0 = code; tile.kp[0] = param; }
+      if (at == 16 + c) { tile.k1 = code; tile.kp[1] = param; }
+      const u32 vcode = HD == 128 ? s_new[1][c] : (s_new[1][c >> 1] >> (16 * (c & 1))) & 0xffff;
+      const u32 vparam = s_newp[1][c * (HD / 16) / KV4_GROUP];
 #pragma unroll
       for (int n = 0; n < 8; ++n)
-        if (at == (n & 3) + 4 * h + 16 * (n >> 2)) {
-          tile.v[n] = HD == 128 ? s_new[1][c] : (s_new[1][c >> 1] >> (16 * (c & 1))) & 0xffff;
-          tile.vp[n] = s_newp[1][c * (HD / 16) / KV4_GROUP];
-        }
+        if (at == kv4_key(n, h)) { tile.v[n] = vcode; tile.vp[n] = vparam; }
     }
-    f4 sc[2];
-    kv4_scores<HD>(tile, query, sc);
-    float x[8], top = -INFINITY;
+    f4 s0, s1;
+    kv4_scores<HD>(tile, query, s0, s1);
+    s0 *= query.scale;
+    s1 *= query.scale;
+    if (u0 + KV4_TILE - 1 > first_limit || ~there_mask) {                  // some query does not see some key
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = sc[i >> 2][i & 3] * query.scale;
-    int low = tile.row[0];
-#pragma unroll
-    for (int i = 1; i < 8; ++i) low = min(low, tile.row[i]);
-    if (u0 + KV4_TILE - 1 > first_limit || __any(low < 0)) {               // some query does not see some key
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (tile.row[i] < 0 || u0 + (i & 3) + 4 * h + 16 * (i >> 2) > limit) x[i] = -INFINITY;
+      for (int i = 0; i < 4; ++i) {
+        const int a = kv4_key(i, h), b = kv4_key(4 + i, h);
+        if (!(there_mask >> a & 1) || u0 + a > limit) s0[i] = -INFINITY;
+        if (!(there_mask >> b & 1) || u0 + b > limit) s1[i] = -INFINITY;
+      }
     }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) top = fmaxf(top, x[i]);
+    float top = fmaxf(fmaxf(fmaxf(s0[0], s0[1]), fmaxf(s0[2], s0[3])), fmaxf(fmaxf(s1[0], s1[1]), fmaxf(s1[2], s1[3])));
     top = fmaxf(kv4_max_over_quarters(top), m);
     if (__any(top > m)) {
       const float corr = top > m ? __builtin_amdgcn_exp2f(m - top) : 1.0f;
@@ -587,40 +592,47 @@ __global__ __launch_bounds__(256) void kv4_attn_few_kernel(Kv4Pool p, Kv4Rows r,
       for (int e = 0; e <= NE; ++e) acc[e] *= corr;
     }
     const float base = (m > -INFINITY ? m : 0.f) - KV4_SHIFT;
-    h8 ph, pl;
+    u32x4 ph, pl;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float v = __builtin_amdgcn_exp2f(x[i] - base);
-      ph[i] = (half_t)v;
-      pl[i] = (half_t)(v - (float)ph[i]);
+    for (int i = 0; i < 4; ++i) {
+      const f4& x = i < 2 ? s0 : s1;
+      const float a = __builtin_amdgcn_exp2f(x[2 * (i & 1)] - base), b = __builtin_amdgcn_exp2f(x[2 * (i & 1) + 1] - base);
+      const h2 hi{(half_t)a, (half_t)b};
+      ph[i] = kv4_u32(hi);
+      pl[i] = kv4_u32(h2{(half_t)(a - (float)hi[0]), (half_t)(b - (float)hi[1])});
     }
     h8 op[NE + 1];
-    kv4_value_operands<HD>(tile, c, op);
+    kv4_value_operands<HD>(tile, there_mask, c, h, op);
 #pragma unroll
     for (int e = 0; e <= NE; ++e) {
-      acc[e] = kv4_mfma(op[e], ph, acc[e]);
-      acc[e] = kv4_mfma(op[e], pl, acc[e]);
+      acc[e] = kv4_mfma(op[e], __builtin_bit_cast(h8, ph), acc[e]);
+      acc[e] = kv4_mfma(op[e], __builtin_bit_cast(h8, pl), acc[e]);
     }
   };
 
-  Kv4Tile<HD> a, b;
-  int t = t0 + wave;
+  // Two tiles are in flight: the next one's loads are out before a tile is used
+  Kv4Tile<HD> ta, tb;
+  u32 ma, mb;
+  int t = t0 + wave, at = 0;
   if (t < t1) {
-    look(t, 0);
-    keys.load(s_rows[wave][0], h, c, a);
+    ma = row(t, look(t), 0);
+    at = look(t + KV4_WAVES);
+    keys.load(s_rows[wave][0], h, c, ta);
   }
   for (; t < t1; t += 2 * KV4_WAVES) {
-    if (t + KV4_WAVES < t1) {
-      look(t + KV4_WAVES, 1);
-      keys.load(s_rows[wave][1], h, c, b);
-    }
-    use(t, a);
+    mb = row(t + KV4_WAVES, at, 1);
+    at = look(t + 2 * KV4_WAVES);
+    keys.load(s_rows[wave][1], h, c, tb);
+    __builtin_amdgcn_sched_barrier(0);
+    use(t, ta, ma);
     if (t + KV4_WAVES >= t1) break;
-    if (t + 2 * KV4_WAVES < t1) {
-      look(t + 2 * KV4_WAVES, 0);
-      keys.load(s_rows[wave][0], h, c, a);
-    }
-    use(t + KV4_WAVES, b);
+    __builtin_amdgcn_sched_barrier(0);
+    ma = row(t + 2 * KV4_WAVES, at, 0);
+    at = look(t + 3 * KV4_WAVES);
+    keys.load(s_rows[wave][0], h, c, ta);
+    __builtin_amdgcn_sched_barrier(0);
+    use(t + KV4_WAVES, tb, mb);
+    __builtin_amdgcn_sched_barrier(0);
   }
 
   // the waves' softmaxes meet
