@@ -285,13 +285,22 @@ __device__ __forceinline__ u32 kv4_hi16(u32 a, u32 b) { return __builtin_amdgcn_
 
 // Nibbles 0 and 4, 1 and 5, 2 and 6, 3 and 7 of w as pairs of c - 8: a code set into the mantissa of 1024 (or, four bits
 // higher, of 64) is that number plus c.
-__device__ __forceinline__ void kv4_unpack(u32 w, h2 (&d)[4]) {
-  const u32 y = w >> 8;
-  d[0] = kv4_h2((w & 0x000f000fu) | 0x64006400u) - h2{1032, 1032};
-  d[1] = kv4_h2((w & 0x00f000f0u) | 0x54005400u) - h2{72, 72};
-  d[2] = kv4_h2((y & 0x000f000fu) | 0x64006400u) - h2{1032, 1032};
-  d[3] = kv4_h2((y & 0x00f000f0u) | 0x54005400u) - h2{72, 72};
-}
+// The constants are hidden from the compiler, in registers of the two kinds that v_and_or_b32 takes together: it would write
+// two instructions with a literal each.
+struct Kv4Bits {
+  u32 low, high, k1024, k64;
+  __device__ __forceinline__ Kv4Bits() : low(0x000f000fu), high(0x00f000f0u), k1024(0x64006400u), k64(0x54005400u) {
+    asm("" : "+s"(low), "+s"(high));
+    asm("" : "+v"(k1024), "+v"(k64));
+  }
+  __device__ __forceinline__ void unpack(u32 w, h2 (&d)[4]) const {
+    const u32 y = w >> 8;
+    d[0] = kv4_h2((w & low) | k1024) - h2{1032, 1032};
+    d[1] = kv4_h2((w & high) | k64) - h2{72, 72};
+    d[2] = kv4_h2((y & low) | k1024) - h2{1032, 1032};
+    d[3] = kv4_h2((y & high) | k64) - h2{72, 72};
+  }
+};
 
 __device__ __forceinline__ float kv4_max_over_quarters(float v) {      // lanes c, c + 16, c + 32, c + 48
   const u32 b = __builtin_bit_cast(u32, v);
@@ -361,7 +370,7 @@ __device__ __forceinline__ void kv4_load_query(const Kv4View& v, bool there, int
   }
   const half_t s1 = (half_t)sum, s2 = (half_t)(sum - (float)s1), s3 = (half_t)(sum - (float)s1 - (float)s2);
   out.sums = h8{s1, s2, s3, 0, 0, 0, 0, 0};
-  out.scale = ldexpf(scale * 1.44269504088896340736f, e);
+  out.scale = fmaxf(ldexpf(scale * 1.44269504088896340736f, e), 0x1p-126f);
 }
 
 // A tile of 32 keys as it lies in the pool: the lane's part of keys c and 16 + c, and of its 8 values
@@ -391,9 +400,8 @@ struct Kv4Keys {
     return *as_global(reinterpret_cast<const W*>(base + (size_t)(row * bytes + at)));
   }
   // rows: the tile's 32 pool rows in LDS
-  __device__ __forceinline__ void load(const u32* rows, int h, int c, Kv4Tile<HD>& t) const {
+  __device__ __forceinline__ void load_keys(const u32* rows, int c, Kv4Tile<HD>& t) const {
     const u32 r0 = rows[c], r1 = rows[16 + c];
-    const u32x4 a = *reinterpret_cast<const u32x4*>(rows + 4 * h), b = *reinterpret_cast<const u32x4*>(rows + 16 + 4 * h);
     if (HD == 128) {
       t.k0 = get<u32x4>(kc, r0, HD / 2, kc_at);
       t.k1 = get<u32x4>(kc, r1, HD / 2, kc_at);
@@ -403,6 +411,9 @@ struct Kv4Keys {
       t.k1 = u32x4{y[0], y[1], 0, 0};
     }
     t.kp = u32x2{get<u32>(kp, r0, HD / 8, kp_at), get<u32>(kp, r1, HD / 8, kp_at)};
+  }
+  __device__ __forceinline__ void load_values(const u32* rows, int h, Kv4Tile<HD>& t) const {
+    const u32x4 a = *reinterpret_cast<const u32x4*>(rows + 4 * h), b = *reinterpret_cast<const u32x4*>(rows + 16 + 4 * h);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const u32 r = j < 4 ? a[j] : b[j - 4];
@@ -414,7 +425,7 @@ struct Kv4Keys {
 
 // Keys of a tile against the queries: S^T of keys 16 j + 4 h + i
 template <int HD>
-__device__ __forceinline__ void kv4_scores(const Kv4Tile<HD>& t, const Kv4Query<HD>& q, f4& s0, f4& s1) {
+__device__ __forceinline__ void kv4_scores(const Kv4Tile<HD>& t, const Kv4Query<HD>& q, const Kv4Bits& bits, f4& s0, f4& s1) {
   auto one = [&](u32x4 w, u32 param) {
     const half_t mid = kv4_h2(param)[1];
     f4 s = kv4_mfma(h8{mid, mid, mid, 0, 0, 0, 0, 0}, q.sums, f4{0.f, 0.f, 0.f, 0.f});
@@ -422,7 +433,7 @@ __device__ __forceinline__ void kv4_scores(const Kv4Tile<HD>& t, const Kv4Query<
 #pragma unroll
     for (int n = 0; n < HD / 32; ++n) {
       h2 d[4];
-      kv4_unpack(w[n], d);
+      bits.unpack(w[n], d);
       const u32x4 a{kv4_u32(d[0] * step), kv4_u32(d[1] * step), kv4_u32(d[2] * step), kv4_u32(d[3] * step)};
       s = kv4_mfma(__builtin_bit_cast(h8, a), q.q[n], s);
     }
@@ -435,12 +446,11 @@ __device__ __forceinline__ void kv4_scores(const Kv4Tile<HD>& t, const Kv4Query<
 // Bit of the lane's i-th key (keys 4 h .. and 16 + 4 h ..) in a word with a bit for each of a tile's keys
 __device__ __forceinline__ int kv4_key(int i, int h) { return (i & 3) + 4 * h + 16 * (i >> 2); }
 
-// Values of a tile as operands: o[e] is row block e (element (HD / 16) c + e of the lane's 8 keys), o[HD / 16] the block
-// of middles, ones and NaN marks.  there: which of the tile's keys have a row.
+// Operand of the block of middles, ones and NaN marks.  there: which of the tile's keys have a row.  Keys that have none, and
+// groups that are NaN, must not meet a weight of zero: their parameters become zero.  Both are rare and found for the whole wave
+// at once: a sum of all middles is NaN if one is.
 template <int HD>
-__device__ __forceinline__ void kv4_value_operands(Kv4Tile<HD>& t, u32 there, int c, int h, h8 (&o)[HD / 16 + 1]) {
-  // Keys that are not there, and groups that are NaN, must not meet a weight of zero.  Both are rare and found for the whole
-  // wave at once: a sum of all middles is NaN if one is.
+__device__ __forceinline__ h8 kv4_middles(Kv4Tile<HD>& t, u32 there, int c, int h) {
   u32 marks = 0;
   h2 all = kv4_h2(t.vp[0]);
 #pragma unroll
@@ -454,31 +464,31 @@ __device__ __forceinline__ void kv4_value_operands(Kv4Tile<HD>& t, u32 there, in
       if (gone || nan) t.vp[j] = 0;
     }
   }
-  u32x4 w[HD / 16 + 1];
+  u32x4 w;
+  const u32 fill = c == 1 ? 0x3c003c00u : 0u;
+#pragma unroll
+  for (int a = 0; a < 4; ++a) w[a] = (c & 3) == 0 ? kv4_hi16(t.vp[2 * a], t.vp[2 * a + 1]) : fill;
+  if (marks && (c & 3) == 2) {
+#pragma unroll
+    for (int a = 0; a < 4; ++a) w[a] = (marks >> (2 * a) & 1 ? 0x3c00u : 0u) | (marks >> (2 * a + 1) & 1 ? 0x3c000000u : 0u);
+  }
+  return __builtin_bit_cast(h8, w);
+}
+
+// Values of a tile as operands: o[i] is row block 4 PART + i (element (HD / 16) c + 4 PART + i of the lane's 8 keys)
+template <int HD, int PART>
+__device__ __forceinline__ void kv4_values(const Kv4Tile<HD>& t, const Kv4Bits& bits, h8 (&o)[4]) {
+  u32x4 w[4];
 #pragma unroll
   for (int a = 0; a < 4; ++a) {
     const h2 step = kv4_h2(kv4_lo16(t.vp[2 * a], t.vp[2 * a + 1]));
-    w[HD / 16][a] = kv4_hi16(t.vp[2 * a], t.vp[2 * a + 1]);
     h2 d[4];
-    kv4_unpack(kv4_lo16(t.v[2 * a], t.v[2 * a + 1]), d);
+    bits.unpack(PART ? kv4_hi16(t.v[2 * a], t.v[2 * a + 1]) : kv4_lo16(t.v[2 * a], t.v[2 * a + 1]), d);
 #pragma unroll
     for (int i = 0; i < 4; ++i) w[i][a] = kv4_u32(d[i] * step);
-    if (HD == 128) {
-      kv4_unpack(kv4_hi16(t.v[2 * a], t.v[2 * a + 1]), d);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) w[4 * (HD / 128) + i][a] = kv4_u32(d[i] * step);
-    }
-  }
-  const u32 fill = c == 1 ? 0x3c003c00u : 0u;
-#pragma unroll
-  for (int a = 0; a < 4; ++a) w[HD / 16][a] = (c & 3) == 0 ? w[HD / 16][a] : fill;
-  if (marks && (c & 3) == 2) {
-#pragma unroll
-    for (int a = 0; a < 4; ++a)
-      w[HD / 16][a] = (marks >> (2 * a) & 1 ? 0x3c00u : 0u) | (marks >> (2 * a + 1) & 1 ? 0x3c000000u : 0u);
   }
 #pragma unroll
-  for (int e = 0; e <= HD / 16; ++e) o[e] = __builtin_bit_cast(h8, w[e]);
+  for (int i = 0; i < 4; ++i) o[i] = __builtin_bit_cast(h8, w[i]);
 }
 
 // Up to 16 query rows of one key head.  grid = splits * kv_heads * row blocks * sequences workgroups (kv4_work's order) of four
@@ -486,7 +496,7 @@ __device__ __forceinline__ void kv4_value_operands(Kv4Tile<HD>& t, u32 there, in
 // NEW: knew and vnew hold the sequences' last rows (one row each), which the workgroup that has the last key quantises into
 // the pool and attends from LDS.  part: with more than one split, the shares' results ([work][16][HD + 2] floats).
 template <class T, int HD, bool NEW>
-__global__ __launch_bounds__(256, 2) void kv4_attn_few_kernel(Kv4Pool p, Kv4Rows r, Kv4View q, Kv4View o, Kv4View knew, Kv4View vnew,
+__global__ __launch_bounds__(256, 3) void kv4_attn_few_kernel(Kv4Pool p, Kv4Rows r, Kv4View q, Kv4View o, Kv4View knew, Kv4View vnew,
                                                            int heads, float scale, int splits, int row_blocks, float* part) {
   constexpr int NE = HD / 16;
   struct Meet { float acc[KV4_WAVES][NE + 1][64][4]; };
@@ -556,83 +566,88 @@ __global__ __launch_bounds__(256, 2) void kv4_attn_few_kernel(Kv4Pool p, Kv4Rows
   for (int e = 0; e <= NE; ++e) acc[e] = f4{0.f, 0.f, 0.f, 0.f};
   float m = -INFINITY;
 
-  auto use = [&](int t, Kv4Tile<HD>& tile, u32 there_mask) {
+  // One tile's registers: the next tile's keys are requested as soon as the scores are there, its values as soon as this
+  // tile's are operands.
+  const Kv4Bits bits;
+  Kv4Tile<HD> tile;
+  int t = t0 + wave, at = 0;
+  u32 has = 0;                                                             // keys of the tile that have a row
+  if (t < t1) {
+    has = row(t, look(t), 0);
+    at = look(t + KV4_WAVES);
+    keys.load_keys(s_rows[wave][0], c, tile);
+    keys.load_values(s_rows[wave][0], h, tile);
+  }
+  for (int buf = 1; t < t1; t += KV4_WAVES, buf ^= 1) {
     const int u0 = t * KV4_TILE;
+    const u32* next = s_rows[wave][buf];
+    const u32 next_has = row(t + KV4_WAVES, at, buf);
+    at = look(t + 2 * KV4_WAVES);
     if (NEW && pnew >= u0 && pnew < u0 + KV4_TILE) {
-      const int at = pnew - u0;
+      const int n0 = pnew - u0;
       const u32x4 code = HD == 128 ? *reinterpret_cast<const u32x4*>(&s_new[0][h * (HD / 32)])
                                    : u32x4{s_new[0][2 * h], s_new[0][2 * h + 1], 0, 0};
       const u32 param = s_newp[0][HD == 128 ? h : h >> 1];
-      if (at == c) { tile.k0 = code; tile.kp[0] = param; }
-      if (at == 16 + c) { tile.k1 = code; tile.kp[1] = param; }
+      if (n0 == c) { tile.k0 = code; tile.kp[0] = param; }
+      if (n0 == 16 + c) { tile.k1 = code; tile.kp[1] = param; }
       const u32 vcode = HD == 128 ? s_new[1][c] : (s_new[1][c >> 1] >> (16 * (c & 1))) & 0xffff;
       const u32 vparam = s_newp[1][c * (HD / 16) / KV4_GROUP];
 #pragma unroll
       for (int n = 0; n < 8; ++n)
-        if (at == kv4_key(n, h)) { tile.v[n] = vcode; tile.vp[n] = vparam; }
+        if (n0 == kv4_key(n, h)) { tile.v[n] = vcode; tile.vp[n] = vparam; }
     }
     f4 s0, s1;
-    kv4_scores<HD>(tile, query, s0, s1);
-    s0 *= query.scale;
-    s1 *= query.scale;
-    if (u0 + KV4_TILE - 1 > first_limit || ~there_mask) {                  // some query does not see some key
+    kv4_scores<HD>(tile, query, bits, s0, s1);
+    __builtin_amdgcn_sched_barrier(0);
+    keys.load_keys(next, c, tile);
+    if (u0 + KV4_TILE - 1 > first_limit || ~has) {                         // some query does not see some key
+      asm volatile("");                                                    // (a branch, not selects in every tile)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int a = kv4_key(i, h), b = kv4_key(4 + i, h);
-        if (!(there_mask >> a & 1) || u0 + a > limit) s0[i] = -INFINITY;
-        if (!(there_mask >> b & 1) || u0 + b > limit) s1[i] = -INFINITY;
+        if (!(has >> a & 1) || u0 + a > limit) s0[i] = -INFINITY;
+        if (!(has >> b & 1) || u0 + b > limit) s1[i] = -INFINITY;
       }
     }
     float top = fmaxf(fmaxf(fmaxf(s0[0], s0[1]), fmaxf(s0[2], s0[3])), fmaxf(fmaxf(s1[0], s1[1]), fmaxf(s1[2], s1[3])));
-    top = fmaxf(kv4_max_over_quarters(top), m);
+    top = fmaxf(kv4_max_over_quarters(top) * query.scale, m);
     if (__any(top > m)) {
       const float corr = top > m ? __builtin_amdgcn_exp2f(m - top) : 1.0f;
       m = top;
 #pragma unroll
       for (int e = 0; e <= NE; ++e) acc[e] *= corr;
     }
-    const float base = (m > -INFINITY ? m : 0.f) - KV4_SHIFT;
+    const float base = KV4_SHIFT - (m > -INFINITY ? m : 0.f);
     u32x4 ph, pl;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const f4& x = i < 2 ? s0 : s1;
-      const float a = __builtin_amdgcn_exp2f(x[2 * (i & 1)] - base), b = __builtin_amdgcn_exp2f(x[2 * (i & 1) + 1] - base);
+      const float a = __builtin_amdgcn_exp2f(fmaf(x[2 * (i & 1)], query.scale, base));
+      const float b = __builtin_amdgcn_exp2f(fmaf(x[2 * (i & 1) + 1], query.scale, base));
       const h2 hi{(half_t)a, (half_t)b};
       ph[i] = kv4_u32(hi);
       pl[i] = kv4_u32(h2{(half_t)(a - (float)hi[0]), (half_t)(b - (float)hi[1])});
     }
-    h8 op[NE + 1];
-    kv4_value_operands<HD>(tile, there_mask, c, h, op);
+    auto add = [&](int e, h8 o) {
+      acc[e] = kv4_mfma(o, __builtin_bit_cast(h8, ph), acc[e]);
+      acc[e] = kv4_mfma(o, __builtin_bit_cast(h8, pl), acc[e]);
+    };
+    add(NE, kv4_middles<HD>(tile, has, c, h));
+    h8 op[4];
+    kv4_values<HD, 0>(tile, bits, op);
 #pragma unroll
-    for (int e = 0; e <= NE; ++e) {
-      acc[e] = kv4_mfma(op[e], __builtin_bit_cast(h8, ph), acc[e]);
-      acc[e] = kv4_mfma(op[e], __builtin_bit_cast(h8, pl), acc[e]);
+    for (int i = 0; i < 4; ++i) add(i, op[i]);
+    if (HD == 128) {
+      kv4_values<HD, 1>(tile, bits, op);
+      __builtin_amdgcn_sched_barrier(0);
+      keys.load_values(next, h, tile);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) add(4 * (HD / 128) + i, op[i]);
+    } else {
+      __builtin_amdgcn_sched_barrier(0);
+      keys.load_values(next, h, tile);
     }
-  };
-
-  // Two tiles are in flight: the next one's loads are out before a tile is used
-  Kv4Tile<HD> ta, tb;
-  u32 ma, mb;
-  int t = t0 + wave, at = 0;
-  if (t < t1) {
-    ma = row(t, look(t), 0);
-    at = look(t + KV4_WAVES);
-    keys.load(s_rows[wave][0], h, c, ta);
-  }
-  for (; t < t1; t += 2 * KV4_WAVES) {
-    mb = row(t + KV4_WAVES, at, 1);
-    at = look(t + 2 * KV4_WAVES);
-    keys.load(s_rows[wave][1], h, c, tb);
-    __builtin_amdgcn_sched_barrier(0);
-    use(t, ta, ma);
-    if (t + KV4_WAVES >= t1) break;
-    __builtin_amdgcn_sched_barrier(0);
-    ma = row(t + 2 * KV4_WAVES, at, 0);
-    at = look(t + 3 * KV4_WAVES);
-    keys.load(s_rows[wave][0], h, c, ta);
-    __builtin_amdgcn_sched_barrier(0);
-    use(t + KV4_WAVES, tb, mb);
-    __builtin_amdgcn_sched_barrier(0);
+    has = next_has;
   }
 
   // the waves' softmaxes meet
