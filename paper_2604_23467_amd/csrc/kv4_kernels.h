@@ -98,10 +98,12 @@ __device__ __forceinline__ int kv4_row(const Kv4Pool& p, const int* table, int t
 
 // ---- element types at the borders: binary16 and bfloat16 ----
 struct Kv4F16 {
+  static constexpr int bits = 11;
   static __device__ __forceinline__ float load(u16 v) { return (float)__builtin_bit_cast(half_t, v); }
   static __device__ __forceinline__ u16 store(float v) { return __builtin_bit_cast(u16, (half_t)v); }
 };
 struct Kv4Bf16 {
+  static constexpr int bits = 8;
   static __device__ __forceinline__ float load(u16 v) { return __builtin_bit_cast(float, (u32)v << 16); }
   static __device__ __forceinline__ u16 store(float v) {      // to the nearest, half to even; NaN stays one
     const u32 b = __builtin_bit_cast(u32, v);
@@ -268,8 +270,9 @@ __global__ __launch_bounds__(256) void kv4_read_kernel(Kv4Pool p, Kv4Rows r, Kv4
 //    (HD / 16) c + e.  A further product's rows are the middles of the groups (row 4 g'), ones (row 1: the sum of the
 //    weights) and where a group is NaN (rows 4 g' + 2); a lane's outputs then all belong to one group, whose sum is in its
 //    own registers.
-// s (c - 8) is exact in binary16 (see above).  Weights are at most 2^15 (the maximum is taken off in front of the exponential)
-// and enter as two binary16 numbers, so that they count with 22 bits; sums are 32 bits wide.
+// s (c - 8) is exact in binary16 (see above).  Weights are at most 2^15 (the maximum is taken off in front of the exponential);
+// they enter as two binary16 numbers, which is 22 bits, where outputs are binary16 themselves, and as one, 11 bits, where these
+// have 8; sums are 32 bits wide.
 
 typedef half_t h2 __attribute__((ext_vector_type(2)));
 
@@ -499,6 +502,7 @@ template <class T, int HD, bool NEW>
 __global__ __launch_bounds__(256, 3) void kv4_attn_few_kernel(Kv4Pool p, Kv4Rows r, Kv4View q, Kv4View o, Kv4View knew, Kv4View vnew,
                                                            int heads, float scale, int splits, int row_blocks, float* part) {
   constexpr int NE = HD / 16;
+  constexpr bool TWO = T::bits > 8;
   struct Meet { float acc[KV4_WAVES][NE + 1][64][4]; };
   __shared__ union {
     Meet meet;
@@ -598,10 +602,11 @@ __global__ __launch_bounds__(256, 3) void kv4_attn_few_kernel(Kv4Pool p, Kv4Rows
     }
     f4 s0, s1;
     kv4_scores<HD>(tile, query, bits, s0, s1);
+    s0 *= query.scale;
+    s1 *= query.scale;
     __builtin_amdgcn_sched_barrier(0);
     keys.load_keys(next, c, tile);
     if (u0 + KV4_TILE - 1 > first_limit || ~has) {                         // some query does not see some key
-      asm volatile("");                                                    // (a branch, not selects in every tile)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int a = kv4_key(i, h), b = kv4_key(4 + i, h);
@@ -610,7 +615,7 @@ __global__ __launch_bounds__(256, 3) void kv4_attn_few_kernel(Kv4Pool p, Kv4Rows
       }
     }
     float top = fmaxf(fmaxf(fmaxf(s0[0], s0[1]), fmaxf(s0[2], s0[3])), fmaxf(fmaxf(s1[0], s1[1]), fmaxf(s1[2], s1[3])));
-    top = fmaxf(kv4_max_over_quarters(top) * query.scale, m);
+    top = fmaxf(kv4_max_over_quarters(top), m);
     if (__any(top > m)) {
       const float corr = top > m ? __builtin_amdgcn_exp2f(m - top) : 1.0f;
       m = top;
@@ -622,15 +627,19 @@ __global__ __launch_bounds__(256, 3) void kv4_attn_few_kernel(Kv4Pool p, Kv4Rows
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const f4& x = i < 2 ? s0 : s1;
-      const float a = __builtin_amdgcn_exp2f(fmaf(x[2 * (i & 1)], query.scale, base));
-      const float b = __builtin_amdgcn_exp2f(fmaf(x[2 * (i & 1) + 1], query.scale, base));
-      const h2 hi{(half_t)a, (half_t)b};
-      ph[i] = kv4_u32(hi);
-      pl[i] = kv4_u32(h2{(half_t)(a - (float)hi[0]), (half_t)(b - (float)hi[1])});
+      const float a = __builtin_amdgcn_exp2f(x[2 * (i & 1)] + base);
+      const float b = __builtin_amdgcn_exp2f(x[2 * (i & 1) + 1] + base);
+      if (TWO) {                                                           // cut to 11 bits, and what that leaves, cut likewise
+        const auto hi = __builtin_amdgcn_cvt_pkrtz(a, b);
+        ph[i] = __builtin_bit_cast(u32, hi);
+        pl[i] = __builtin_bit_cast(u32, __builtin_amdgcn_cvt_pkrtz(fmaf((float)hi[0], -1.0f, a), fmaf((float)hi[1], -1.0f, b)));
+      } else {
+        ph[i] = kv4_u32(h2{(half_t)a, (half_t)b});
+      }
     }
     auto add = [&](int e, h8 o) {
       acc[e] = kv4_mfma(o, __builtin_bit_cast(h8, ph), acc[e]);
-      acc[e] = kv4_mfma(o, __builtin_bit_cast(h8, pl), acc[e]);
+      if (TWO) acc[e] = kv4_mfma(o, __builtin_bit_cast(h8, pl), acc[e]);
     };
     add(NE, kv4_middles<HD>(tile, has, c, h));
     h8 op[4];
