@@ -116,10 +116,12 @@ void kv4_launch_attention(hipStream_t s, int32_t dtype, int head_dim, const Kv4P
     using T = decltype(t);
     constexpr int HD = decltype(hd)::value;
     const dim3 grid((unsigned)(a.works * a.splits));
-    if (k && r.max_rows == 1)
-      hipLaunchKernelGGL((kv4_attn_few_kernel<T, HD, true>), grid, dim3(256), 0, s, p, r, q, o, *k, *v, heads, scale, a.splits, a.row_blocks, part);
-    else
-      hipLaunchKernelGGL((kv4_attn_few_kernel<T, HD, false>), grid, dim3(256), 0, s, p, r, q, o, q, q, heads, scale, a.splits, a.row_blocks, part);
+    const bool p16 = p.page_tokens % 16 == 0, fresh = k && r.max_rows == 1;
+    auto go = [&](auto kernel) {
+      hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, p, r, q, o, fresh ? *k : q, fresh ? *v : q, heads, scale, a.splits, a.row_blocks, part);
+    };
+    if (p16) fresh ? go(kv4_attn_few_kernel<T, HD, true, true>) : go(kv4_attn_few_kernel<T, HD, true, false>);
+    else fresh ? go(kv4_attn_few_kernel<T, HD, false, true>) : go(kv4_attn_few_kernel<T, HD, false, false>);
     if (a.splits > 1)
       hipLaunchKernelGGL((kv4_join_kernel<T, HD>), dim3((unsigned)a.works), dim3(256), 0, s, p, r, o, heads, a.splits, a.row_blocks, part);
   });

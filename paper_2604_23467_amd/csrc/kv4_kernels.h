@@ -88,6 +88,9 @@ __device__ __forceinline__ int kv4_find(const Kv4Rows& r, int i) {
   return -1;
 }
 
+// An entry of the page table at an address that all lanes share
+__device__ __forceinline__ int kv4_scalar(const int* p) { return *(const __attribute__((address_space(4))) int*)p; }
+
 // Pool row of position u >= 0 of the sequence with this page-table row; -1 where there is none
 __device__ __forceinline__ int kv4_row(const Kv4Pool& p, const int* table, int table_stride, int u) {
   const int page = (int)(__umulhi((u32)u << 1, p.magic) >> p.shift);
@@ -388,7 +391,8 @@ template <int HD>
 struct Kv4Keys {
   const char *kc, *kp, *vc, *vp;      // codes and parameters of the key head
   u32 kc_at, kp_at, vc_at, vp_at;     // the lane's part of a row
-  __device__ __forceinline__ Kv4Keys(const Kv4Pool& p, int head, int h, int c) {
+  int h, c;
+  __device__ __forceinline__ Kv4Keys(const Kv4Pool& p, int head, int h_, int c_) : h(h_), c(c_) {
     kc = kv4_codes<HD>(p, 0, head);
     kp = kv4_params<HD>(p, 0, head);
     vc = kv4_codes<HD>(p, 1, head);
@@ -399,29 +403,49 @@ struct Kv4Keys {
     vp_at = (c * (HD / 16) / KV4_GROUP) * 4;
   }
   template <class W>
-  static __device__ __forceinline__ W get(const char* base, u32 row, u32 bytes, u32 at) {
-    return *as_global(reinterpret_cast<const W*>(base + (size_t)(row * bytes + at)));
+  static __device__ __forceinline__ W get(const char* base, u32 at) {
+    return *as_global(reinterpret_cast<const W*>(base + (size_t)at));
   }
-  // rows: the tile's 32 pool rows in LDS
-  __device__ __forceinline__ void load_keys(const u32* rows, int c, Kv4Tile<HD>& t) const {
-    const u32 r0 = rows[c], r1 = rows[16 + c];
+  __device__ __forceinline__ void set_keys(const char* c0, u32 o0, const char* c1, u32 o1, const char* p0, u32 q0, const char* p1, u32 q1,
+                                           Kv4Tile<HD>& t) const {
     if (HD == 128) {
-      t.k0 = get<u32x4>(kc, r0, HD / 2, kc_at);
-      t.k1 = get<u32x4>(kc, r1, HD / 2, kc_at);
+      t.k0 = get<u32x4>(c0, o0);
+      t.k1 = get<u32x4>(c1, o1);
     } else {
-      const u32x2 x = get<u32x2>(kc, r0, HD / 2, kc_at), y = get<u32x2>(kc, r1, HD / 2, kc_at);
+      const u32x2 x = get<u32x2>(c0, o0), y = get<u32x2>(c1, o1);
       t.k0 = u32x4{x[0], x[1], 0, 0};
       t.k1 = u32x4{y[0], y[1], 0, 0};
     }
-    t.kp = u32x2{get<u32>(kp, r0, HD / 8, kp_at), get<u32>(kp, r1, HD / 8, kp_at)};
+    t.kp = u32x2{get<u32>(p0, q0), get<u32>(p1, q1)};
   }
-  __device__ __forceinline__ void load_values(const u32* rows, int h, Kv4Tile<HD>& t) const {
+  // rows: a tile's 32 pool rows in LDS
+  __device__ __forceinline__ void load_keys(const u32* rows, Kv4Tile<HD>& t) const {
+    const u32 r0 = rows[c], r1 = rows[16 + c];
+    set_keys(kc, r0 * (HD / 2) + kc_at, kc, r1 * (HD / 2) + kc_at, kp, r0 * (HD / 8) + kp_at, kp, r1 * (HD / 8) + kp_at, t);
+  }
+  __device__ __forceinline__ void load_values(const u32* rows, Kv4Tile<HD>& t) const {
     const u32x4 a = *reinterpret_cast<const u32x4*>(rows + 4 * h), b = *reinterpret_cast<const u32x4*>(rows + 16 + 4 * h);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const u32 r = j < 4 ? a[j] : b[j - 4];
-      t.v[j] = HD == 128 ? get<u32>(vc, r, HD / 2, vc_at) : (u32)get<u16>(vc, r, HD / 2, vc_at);
-      t.vp[j] = get<u32>(vp, r, HD / 8, vp_at);
+      const u32 r = j < 4 ? a[j] : b[j - 4], x = r * (HD / 2) + vc_at;
+      t.v[j] = HD == 128 ? get<u32>(vc, x) : (u32)get<u16>(vc, x);
+      t.vp[j] = get<u32>(vp, r * (HD / 8) + vp_at);
+    }
+  }
+  // The halves of a tile lie in 16 consecutive pool rows each, from r0 and r1 on (in scalar registers): no lane has an
+  // address to work out
+  __device__ __forceinline__ void load_keys(u32x2 r, Kv4Tile<HD>& t) const {
+    const u32 o = c * (HD / 2) + kc_at, q = c * (HD / 8) + kp_at;
+    set_keys(kc + (size_t)r[0] * (HD / 2), o, kc + (size_t)r[1] * (HD / 2), o, kp + (size_t)r[0] * (HD / 8), q,
+             kp + (size_t)r[1] * (HD / 8), q, t);
+  }
+  __device__ __forceinline__ void load_values(u32x2 r, Kv4Tile<HD>& t) const {
+    const u32 o = 4 * h * (HD / 2) + vc_at, q = 4 * h * (HD / 8) + vp_at;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const char *a = vc + (size_t)r[j >> 2] * (HD / 2) + (j & 3) * (HD / 2), *b = vp + (size_t)r[j >> 2] * (HD / 8) + (j & 3) * (HD / 8);
+      t.v[j] = HD == 128 ? get<u32>(a, o) : (u32)get<u16>(a, o);
+      t.vp[j] = get<u32>(b, q);
     }
   }
 };
@@ -496,9 +520,10 @@ __device__ __forceinline__ void kv4_values(const Kv4Tile<HD>& t, const Kv4Bits& 
 
 // Up to 16 query rows of one key head.  grid = splits * kv_heads * row blocks * sequences workgroups (kv4_work's order) of four
 // waves; the waves take every fourth tile of the workgroup's share and keep a softmax of their own, which meet in LDS.
+// P16: page_tokens is a multiple of 16, so that halves of a tile are consecutive pool rows and their addresses scalar.
 // NEW: knew and vnew hold the sequences' last rows (one row each), which the workgroup that has the last key quantises into
 // the pool and attends from LDS.  part: with more than one split, the shares' results ([work][16][HD + 2] floats).
-template <class T, int HD, bool NEW>
+template <class T, int HD, bool P16, bool NEW>
 __global__ __launch_bounds__(256, 3) void kv4_attn_few_kernel(Kv4Pool p, Kv4Rows r, Kv4View q, Kv4View o, Kv4View knew, Kv4View vnew,
                                                            int heads, float scale, int splits, int row_blocks, float* part) {
   constexpr int NE = HD / 16;
@@ -530,17 +555,37 @@ __global__ __launch_bounds__(256, 3) void kv4_attn_few_kernel(Kv4Pool p, Kv4Rows
 
   const Kv4Keys<HD> keys(p, w.head, h, c);
   // Pool rows of a tile: the page table's entries are requested a tile ahead of the tile's own loads, so that the wait for them
-  // leaves those in flight; row() then leaves the rows in LDS (0 where there is none) and returns which keys have one.
-  const int ahead = lane & (KV4_TILE - 1);
-  auto page = [&](int t) { return (int)(__umulhi((u32)(t * KV4_TILE + ahead) << 1, p.magic) >> p.shift); };
-  auto look = [&](int t) { return *as_global(table + min(page(t), r.table_stride - 1)); };
-  auto row = [&](int t, int at, int buf) {
-    const int u = t * KV4_TILE + ahead, pg = page(t);
-    const bool ok = u < n_keys && pg < r.table_stride && (u32)at <= (u32)(p.pool_rows - p.page_tokens);
-    s_rows[wave][buf][ahead] = ok ? at + (u - pg * p.page_tokens) : 0;
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    return (u32)__ballot(ok);
+  // leaves those in flight.  place() then says where the rows are, and which of the tile's keys have one (others: row 0).
+  // Without P16 a lane looks after a key, and the rows go through LDS.
+  const int ahead = P16 ? 0 : lane & (KV4_TILE - 1);
+  auto page = [&](int u) { return (int)(__umulhi((u32)u << 1, p.magic) >> p.shift); };
+  auto look = [&](int t) {
+    const int last = r.table_stride - 1, u = t * KV4_TILE + ahead;
+    if constexpr (P16) return u32x2{(u32)kv4_scalar(table + min(page(u), last)), (u32)kv4_scalar(table + min(page(u + 16), last))};
+    else return u32x2{(u32)*as_global(table + min(page(u), last)), 0};
+  };
+  auto row = [&](int u, u32 at, u32& out) {
+    const int pg = page(u);
+    const bool ok = u < n_keys && pg < r.table_stride && at <= (u32)(p.pool_rows - p.page_tokens);
+    out = ok ? at + (u - pg * p.page_tokens) : 0;
+    return ok;
+  };
+  auto place = [&](int t, u32x2 at, int buf, u32& has) {
+    const int u = t * KV4_TILE + ahead;
+    if constexpr (P16) {
+      u32 a, b;
+      const u32 one = row(u, at[0], a) ? 0xffffu >> max(u + 16 - n_keys, 0) : 0u;
+      const u32 two = row(u + 16, at[1], b) ? 0xffffu >> max(u + 32 - n_keys, 0) : 0u;
+      has = one | two << 16;
+      return u32x2{a, b};
+    } else {
+      u32 a;
+      has = (u32)__ballot(row(u, at[0], a));
+      s_rows[wave][buf][ahead] = a;
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      return (const u32*)s_rows[wave][buf];
+    }
   };
 
   Kv4Query<HD> query;
@@ -574,18 +619,19 @@ __global__ __launch_bounds__(256, 3) void kv4_attn_few_kernel(Kv4Pool p, Kv4Rows
   // tile's are operands.
   const Kv4Bits bits;
   Kv4Tile<HD> tile;
-  int t = t0 + wave, at = 0;
+  int t = t0 + wave;
+  u32x2 at{0, 0};
   u32 has = 0;                                                             // keys of the tile that have a row
   if (t < t1) {
-    has = row(t, look(t), 0);
+    const auto first = place(t, look(t), 0, has);
     at = look(t + KV4_WAVES);
-    keys.load_keys(s_rows[wave][0], c, tile);
-    keys.load_values(s_rows[wave][0], h, tile);
+    keys.load_keys(first, tile);
+    keys.load_values(first, tile);
   }
   for (int buf = 1; t < t1; t += KV4_WAVES, buf ^= 1) {
     const int u0 = t * KV4_TILE;
-    const u32* next = s_rows[wave][buf];
-    const u32 next_has = row(t + KV4_WAVES, at, buf);
+    u32 next_has;
+    const auto next = place(t + KV4_WAVES, at, buf, next_has);
     at = look(t + 2 * KV4_WAVES);
     if (NEW && pnew >= u0 && pnew < u0 + KV4_TILE) {
       const int n0 = pnew - u0;
@@ -605,7 +651,7 @@ __global__ __launch_bounds__(256, 3) void kv4_attn_few_kernel(Kv4Pool p, Kv4Rows
     s0 *= query.scale;
     s1 *= query.scale;
     __builtin_amdgcn_sched_barrier(0);
-    keys.load_keys(next, c, tile);
+    keys.load_keys(next, tile);
     if (u0 + KV4_TILE - 1 > first_limit || ~has) {                         // some query does not see some key
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -649,12 +695,12 @@ __global__ __launch_bounds__(256, 3) void kv4_attn_few_kernel(Kv4Pool p, Kv4Rows
     if (HD == 128) {
       kv4_values<HD, 1>(tile, bits, op);
       __builtin_amdgcn_sched_barrier(0);
-      keys.load_values(next, h, tile);
+      keys.load_values(next, tile);
 #pragma unroll
       for (int i = 0; i < 4; ++i) add(4 * (HD / 128) + i, op[i]);
     } else {
       __builtin_amdgcn_sched_barrier(0);
-      keys.load_values(next, h, tile);
+      keys.load_values(next, tile);
     }
     has = next_has;
   }
