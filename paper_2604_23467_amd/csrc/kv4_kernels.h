@@ -62,17 +62,21 @@ __device__ __forceinline__ char* kv4_params(const Kv4Pool& p, int which, int hea
 struct Kv4Seq {
   int first, rows, len;
 };
+// A word at an address that all lanes share, by a scalar load (for what no kernel of this file writes)
+__device__ __forceinline__ int kv4_scalar(const int* p) { return *(const __attribute__((address_space(4))) int*)p; }
+
 __device__ __forceinline__ Kv4Seq kv4_seq(const Kv4Rows& r, int b) {
   Kv4Seq s;
   s.first = b * r.max_rows;
   s.rows = r.max_rows;
+  const int len = kv4_scalar(r.len + b);
   if (r.row_start) {
-    const int from = r.row_start[b], to = r.row_start[b + 1];
+    const int from = kv4_scalar(r.row_start + b), to = kv4_scalar(r.row_start + b + 1);
     s.first = min(max(from, 0), r.n_rows);
     s.rows = min(max(to, s.first), r.n_rows) - s.first;
   }
-  s.len = max(r.len[b], 0) + r.len_add;
-  if (r.active && !r.active[b]) s.len = 0;
+  s.len = max(len, 0) + r.len_add;
+  if (r.active && !kv4_scalar(r.active + b)) s.len = 0;
   return s;
 }
 
@@ -87,9 +91,6 @@ __device__ __forceinline__ int kv4_find(const Kv4Rows& r, int i) {
   }
   return -1;
 }
-
-// An entry of the page table at an address that all lanes share
-__device__ __forceinline__ int kv4_scalar(const int* p) { return *(const __attribute__((address_space(4))) int*)p; }
 
 // Pool row of position u >= 0 of the sequence with this page-table row; -1 where there is none
 __device__ __forceinline__ int kv4_row(const Kv4Pool& p, const int* table, int table_stride, int u) {
@@ -387,67 +388,111 @@ struct Kv4Tile {
   u32x8 v, vp;
 };
 
+// Tiles come into LDS by direct loads, which cost no registers while they are under way: a wave has two slots of its own, one
+// of which is filled while the other is used.  A half of a slot (keys or values) is 32 rows of codes in pieces of 16 bytes and
+// their parameters.  Pieces are stored in an order in which neither the keys' reads (a piece of each of 16 rows) nor the
+// values' (a word each of rows 4 h + i) meet in a bank: head_dim 128, piece x of row 4 b + a of a block of 16 rows at
+// 16 b + 4 (a ^ b) + (x ^ b); head_dim 64, piece x of row y at 2 y + (x ^ bit 3 of y).
 template <int HD>
-struct Kv4Keys {
+struct Kv4Ring {
+  static constexpr int CODES = KV4_TILE * HD / 2, PARAMS = KV4_TILE * HD / 8, HALF = CODES + PARAMS, SLOT = 2 * HALF;
+  static constexpr int LOADS = HD == 128 ? 4 : 2;      // direct loads of a half (all lanes take part in each)
   const char *kc, *kp, *vc, *vp;      // codes and parameters of the key head
-  u32 kc_at, kp_at, vc_at, vp_at;     // the lane's part of a row
-  int h, c;
-  __device__ __forceinline__ Kv4Keys(const Kv4Pool& p, int head, int h_, int c_) : h(h_), c(c_) {
+  char* slots;                        // the wave's two slots
+  int lane, h, c;
+  u32 code_row, code_at, param_row, param_at;      // row (of 16, or of 32 with head_dim 64) and bytes in it that the lane brings in
+
+  __device__ __forceinline__ Kv4Ring(const Kv4Pool& p, int head, char* lds, int lane_) : slots(lds), lane(lane_) {
+    h = lane >> 4;
+    c = lane & 15;
     kc = kv4_codes<HD>(p, 0, head);
     kp = kv4_params<HD>(p, 0, head);
     vc = kv4_codes<HD>(p, 1, head);
     vp = kv4_params<HD>(p, 1, head);
-    kc_at = h * (HD / 8);
-    kp_at = (HD == 128 ? h : h >> 1) * 4;
-    vc_at = c * (HD / 32);
-    vp_at = (c * (HD / 16) / KV4_GROUP) * 4;
-  }
-  template <class W>
-  static __device__ __forceinline__ W get(const char* base, u32 at) {
-    return *as_global(reinterpret_cast<const W*>(base + (size_t)at));
-  }
-  __device__ __forceinline__ void set_keys(const char* c0, u32 o0, const char* c1, u32 o1, const char* p0, u32 q0, const char* p1, u32 q1,
-                                           Kv4Tile<HD>& t) const {
     if (HD == 128) {
-      t.k0 = get<u32x4>(c0, o0);
-      t.k1 = get<u32x4>(c1, o1);
+      code_row = 4 * h + (((lane >> 2) & 3) ^ h);
+      code_at = ((lane & 3) ^ h) * 16;
+      param_row = lane >> 2;
+      param_at = (lane & 3) * 4;
     } else {
-      const u32x2 x = get<u32x2>(c0, o0), y = get<u32x2>(c1, o1);
+      code_row = lane >> 1;
+      code_at = ((lane & 1) ^ (lane >> 4 & 1)) * 16;
+      param_row = lane >> 1;
+      param_at = (lane & 1) * 4;
+    }
+  }
+  static __device__ __forceinline__ int piece(int row, int x) {
+    return HD == 128 ? (row & 16) * 64 + ((row >> 2 & 3) * 16 + ((row ^ row >> 2) & 3) * 4 + (x ^ (row >> 2 & 3))) * 16
+                     : (2 * row + (x ^ (row >> 3 & 1))) * 16;
+  }
+  template <int SIZE>
+  static __device__ __forceinline__ void bring(const char* from, char* to) {
+    if constexpr (SIZE == 16) __builtin_amdgcn_global_load_lds((const LL_GLOBAL void*)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+    else __builtin_amdgcn_global_load_lds((const LL_GLOBAL void*)from, (__attribute__((address_space(3))) void*)to, 4, 0, 0);
+  }
+  // where: says where the tile's rows are in the pool
+  template <class Where>
+  __device__ __forceinline__ void fetch(const char* codes, const char* params, char* to, const Where& where) const {
+    if (HD == 128) {
+      bring<16>(where.at(codes, HD / 2, 0, code_row) + code_at, to);
+      bring<16>(where.at(codes, HD / 2, 1, code_row) + code_at, to + CODES / 2);
+      bring<4>(where.at(params, HD / 8, 0, param_row) + param_at, to + CODES);
+      bring<4>(where.at(params, HD / 8, 1, param_row) + param_at, to + CODES + PARAMS / 2);
+    } else {
+      bring<16>(where.split(codes, HD / 2, code_row) + code_at, to);
+      bring<4>(where.split(params, HD / 8, param_row) + param_at, to + CODES);
+    }
+  }
+  template <class Where>
+  __device__ __forceinline__ void fetch_keys(int slot, const Where& where) const { fetch(kc, kp, slots + slot * SLOT, where); }
+  template <class Where>
+  __device__ __forceinline__ void fetch_values(int slot, const Where& where) const { fetch(vc, vp, slots + slot * SLOT + HALF, where); }
+
+  __device__ __forceinline__ void read_keys(int slot, Kv4Tile<HD>& t) const {
+    const char* s = slots + slot * SLOT;
+    if (HD == 128) {
+      t.k0 = *reinterpret_cast<const u32x4*>(s + piece(c, h));
+      t.k1 = *reinterpret_cast<const u32x4*>(s + piece(16 + c, h));
+    } else {
+      const u32x2 x = *reinterpret_cast<const u32x2*>(s + piece(c, h >> 1) + (h & 1) * 8);
+      const u32x2 y = *reinterpret_cast<const u32x2*>(s + piece(16 + c, h >> 1) + (h & 1) * 8);
       t.k0 = u32x4{x[0], x[1], 0, 0};
       t.k1 = u32x4{y[0], y[1], 0, 0};
     }
-    t.kp = u32x2{get<u32>(p0, q0), get<u32>(p1, q1)};
+    const u32* q = reinterpret_cast<const u32*>(s + CODES);
+    const int g = HD == 128 ? h : h >> 1;
+    t.kp = u32x2{q[c * (HD / 32) + g], q[(16 + c) * (HD / 32) + g]};
   }
-  // rows: a tile's 32 pool rows in LDS
-  __device__ __forceinline__ void load_keys(const u32* rows, Kv4Tile<HD>& t) const {
-    const u32 r0 = rows[c], r1 = rows[16 + c];
-    set_keys(kc, r0 * (HD / 2) + kc_at, kc, r1 * (HD / 2) + kc_at, kp, r0 * (HD / 8) + kp_at, kp, r1 * (HD / 8) + kp_at, t);
-  }
-  __device__ __forceinline__ void load_values(const u32* rows, Kv4Tile<HD>& t) const {
-    const u32x4 a = *reinterpret_cast<const u32x4*>(rows + 4 * h), b = *reinterpret_cast<const u32x4*>(rows + 16 + 4 * h);
+  __device__ __forceinline__ void read_values(int slot, Kv4Tile<HD>& t) const {
+    const char* s = slots + slot * SLOT + HALF;
+    const u32* q = reinterpret_cast<const u32*>(s + CODES);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const u32 r = j < 4 ? a[j] : b[j - 4], x = r * (HD / 2) + vc_at;
-      t.v[j] = HD == 128 ? get<u32>(vc, x) : (u32)get<u16>(vc, x);
-      t.vp[j] = get<u32>(vp, r * (HD / 8) + vp_at);
+      const int row = (j & 3) + 4 * h + 16 * (j >> 2);
+      if (HD == 128) t.v[j] = *reinterpret_cast<const u32*>(s + piece(row, c >> 2) + (c & 3) * 4);
+      else t.v[j] = *reinterpret_cast<const u16*>(s + piece(row, c >> 3) + (c & 7) * 2);
+      t.vp[j] = q[row * (HD / 32) + c * (HD / 16) / KV4_GROUP];
     }
   }
-  // The halves of a tile lie in 16 consecutive pool rows each, from r0 and r1 on (in scalar registers): no lane has an
-  // address to work out
-  __device__ __forceinline__ void load_keys(u32x2 r, Kv4Tile<HD>& t) const {
-    const u32 o = c * (HD / 2) + kc_at, q = c * (HD / 8) + kp_at;
-    set_keys(kc + (size_t)r[0] * (HD / 2), o, kc + (size_t)r[1] * (HD / 2), o, kp + (size_t)r[0] * (HD / 8), q,
-             kp + (size_t)r[1] * (HD / 8), q, t);
+};
+// Where a tile's rows are: 16 consecutive pool rows each from two scalar rows on ...
+struct Kv4Halves {
+  u32x2 row;
+  __device__ __forceinline__ const char* at(const char* base, int bytes, int half, u32 i) const {
+    return base + (size_t)row[half] * bytes + i * bytes;
   }
-  __device__ __forceinline__ void load_values(u32x2 r, Kv4Tile<HD>& t) const {
-    const u32 o = 4 * h * (HD / 2) + vc_at, q = 4 * h * (HD / 8) + vp_at;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const char *a = vc + (size_t)r[j >> 2] * (HD / 2) + (j & 3) * (HD / 2), *b = vp + (size_t)r[j >> 2] * (HD / 8) + (j & 3) * (HD / 8);
-      t.v[j] = HD == 128 ? get<u32>(a, o) : (u32)get<u16>(a, o);
-      t.vp[j] = get<u32>(b, q);
-    }
+  __device__ __forceinline__ const char* split(const char* base, int bytes, u32 i) const {
+    const u32 a = row[0], b = row[1];
+    return base + (size_t)(((i & 16) ? b : a) + (i & 15)) * bytes;
   }
+};
+// ... or anywhere, as 32 words in LDS say
+struct Kv4Listed {
+  const u32* rows;
+  __device__ __forceinline__ const char* at(const char* base, int bytes, int half, u32 i) const {
+    return base + (size_t)rows[16 * half + i] * bytes;
+  }
+  __device__ __forceinline__ const char* split(const char* base, int bytes, u32 i) const { return base + (size_t)rows[i] * bytes; }
 };
 
 // Keys of a tile against the queries: S^T of keys 16 j + 4 h + i
@@ -528,12 +573,10 @@ __global__ __launch_bounds__(256, 3) void kv4_attn_few_kernel(Kv4Pool p, Kv4Rows
                                                            int heads, float scale, int splits, int row_blocks, float* part) {
   constexpr int NE = HD / 16;
   constexpr bool TWO = T::bits > 8;
-  struct Meet { float acc[KV4_WAVES][NE + 1][64][4]; };
-  __shared__ union {
-    Meet meet;
-    float out[16][HD + 4];
-  } s_mem;
-  __shared__ __attribute__((aligned(16))) u32 s_rows[KV4_WAVES][2][KV4_TILE];
+  using Ring = Kv4Ring<HD>;
+  constexpr int RING = KV4_WAVES * 2 * Ring::SLOT, MEET = KV4_WAVES * (NE + 1) * 64 * 16;
+  __shared__ __attribute__((aligned(16))) char s_mem[RING > MEET ? RING : MEET];      // the tiles, then what the waves hand in
+  __shared__ __attribute__((aligned(16))) u32 s_rows[P16 ? 1 : KV4_WAVES][KV4_TILE];
   __shared__ float s_m[KV4_WAVES][16];
   __shared__ __attribute__((aligned(16))) u32 s_new[2][HD / 8], s_newp[2][HD / 32];
   const Kv4Work w = kv4_work(blockIdx.x, splits, p.kv_heads, row_blocks);
@@ -543,20 +586,17 @@ __global__ __launch_bounds__(256, 3) void kv4_attn_few_kernel(Kv4Pool p, Kv4Rows
   const int share_heads = heads / p.kv_heads, rows = min(s.rows, r.max_rows) * share_heads;
   const int f0 = w.rb * KV4_FEW_ROWS;
   if (f0 >= rows) return;
-  const int f = f0 + c, j = f / share_heads, qhead = w.head * share_heads + f - j * share_heads;
-  const bool there = f < rows;
-  const int limit = there ? s.len - s.rows + j : -1;                       // last position that the lane's query sees
-  const int first_limit = s.len - s.rows + f0 / share_heads;
+  const int first_limit = s.len - s.rows + f0 / share_heads;               // last position that the first query sees
   const int n_keys = max(s.len - s.rows + min(f0 + KV4_FEW_ROWS - 1, rows - 1) / share_heads + 1, 0);
   const int tiles = (n_keys + KV4_TILE - 1) / KV4_TILE, share = kv4_share(tiles, splits);
   const int t0 = w.split * share, t1 = min(t0 + share, tiles);
   if (w.split > 0 && t0 >= tiles) return;
   const int* table = r.table + (size_t)w.b * r.table_stride;
 
-  const Kv4Keys<HD> keys(p, w.head, h, c);
-  // Pool rows of a tile: the page table's entries are requested a tile ahead of the tile's own loads, so that the wait for them
-  // leaves those in flight.  place() then says where the rows are, and which of the tile's keys have one (others: row 0).
-  // Without P16 a lane looks after a key, and the rows go through LDS.
+  // Pool rows of a tile: the page table's entries are requested a tile ahead of the tile's own loads.  place() then says where
+  // the rows are, and which of the tile's keys have one (others: row 0).  Without P16 a lane looks after a key, and the rows go
+  // through LDS.
+  const Ring ring(p, w.head, s_mem + wave * 2 * Ring::SLOT, lane);
   const int ahead = P16 ? 0 : lane & (KV4_TILE - 1);
   auto page = [&](int u) { return (int)(__umulhi((u32)u << 1, p.magic) >> p.shift); };
   auto look = [&](int t) {
@@ -564,30 +604,49 @@ __global__ __launch_bounds__(256, 3) void kv4_attn_few_kernel(Kv4Pool p, Kv4Rows
     if constexpr (P16) return u32x2{(u32)kv4_scalar(table + min(page(u), last)), (u32)kv4_scalar(table + min(page(u + 16), last))};
     else return u32x2{(u32)*as_global(table + min(page(u), last)), 0};
   };
-  auto row = [&](int u, u32 at, u32& out) {
+  auto row = [&](int u, u32 at) {                                          // -1: none
     const int pg = page(u);
-    const bool ok = u < n_keys && pg < r.table_stride && at <= (u32)(p.pool_rows - p.page_tokens);
-    out = ok ? at + (u - pg * p.page_tokens) : 0;
-    return ok;
+    return u < n_keys && pg < r.table_stride && at <= (u32)(p.pool_rows - p.page_tokens) ? (int)(at + (u - pg * p.page_tokens)) : -1;
   };
-  auto place = [&](int t, u32x2 at, int buf, u32& has) {
+  auto place = [&](int t, u32x2 at, u32& has) {
     const int u = t * KV4_TILE + ahead;
     if constexpr (P16) {
-      u32 a, b;
-      const u32 one = row(u, at[0], a) ? 0xffffu >> max(u + 16 - n_keys, 0) : 0u;
-      const u32 two = row(u + 16, at[1], b) ? 0xffffu >> max(u + 32 - n_keys, 0) : 0u;
+      const int a = row(u, at[0]), b = row(u + 16, at[1]);
+      const u32 one = a >= 0 ? 0xffffu >> max(u + 16 - n_keys, 0) : 0u, two = b >= 0 ? 0xffffu >> max(u + 32 - n_keys, 0) : 0u;
       has = one | two << 16;
-      return u32x2{a, b};
+      return Kv4Halves{u32x2{(u32)max(a, 0), (u32)max(b, 0)}};
     } else {
-      u32 a;
-      has = (u32)__ballot(row(u, at[0], a));
-      s_rows[wave][buf][ahead] = a;
+      const int a = row(u, at[0]);
+      has = (u32)__ballot(a >= 0);
+      s_rows[wave][ahead] = max(a, 0);
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       __builtin_amdgcn_wave_barrier();
-      return (const u32*)s_rows[wave][buf];
+      return Kv4Listed{s_rows[wave]};
     }
   };
+  int t = t0 + wave;
+  u32x2 at{0, 0};
+  u32 has = 0, has1 = 0;                                                   // keys of this tile and the next that have a row
+  if (t < t1) {
+    const u32x2 at0 = look(t), at1 = look(t + KV4_WAVES);
+    at = look(t + 2 * KV4_WAVES);
+    {
+      const auto where = place(t, at0, has);
+      ring.fetch_keys(0, where);
+      ring.fetch_values(0, where);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    {
+      const auto where = place(t + KV4_WAVES, at1, has1);
+      ring.fetch_keys(1, where);
+      ring.fetch_values(1, where);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  }
 
+  const int f = f0 + c, j = f / share_heads, qhead = w.head * share_heads + f - j * share_heads;
+  const bool there = f < rows;
+  const int limit = there ? s.len - s.rows + j : -1;                       // last position that the lane's query sees
   Kv4Query<HD> query;
   kv4_load_query<T, HD>(q, there, s.first + j, qhead, h, scale, query);
   const int pnew = NEW ? s.len - s.rows : -1;
@@ -601,13 +660,15 @@ __global__ __launch_bounds__(256, 3) void kv4_attn_few_kernel(Kv4Pool p, Kv4Rows
       const u32 code = kv4_quantise(x, param);
       s_new[wave][lane] = code;
       s_newp[wave][lane >> 2] = param;
-      const int row = kv4_row(p, table, r.table_stride, pnew);
-      if (row >= 0) {
-        *(u32*)(kv4_codes<HD>(p, wave, w.head) + (size_t)row * (HD / 2) + lane * 4) = code;
-        if (lane % 4 == 0) *(u32*)(kv4_params<HD>(p, wave, w.head) + (size_t)row * (HD / 8) + lane) = param;
+      const int to = kv4_row(p, table, r.table_stride, pnew);
+      if (to >= 0) {
+        *(u32*)(kv4_codes<HD>(p, wave, w.head) + (size_t)to * (HD / 2) + lane * 4) = code;
+        if (lane % 4 == 0) *(u32*)(kv4_params<HD>(p, wave, w.head) + (size_t)to * (HD / 8) + lane) = param;
       }
     }
-    __syncthreads();
+    wait_lgkm_at_most<0>();
+    __builtin_amdgcn_s_barrier();                                          // (__syncthreads would wait for the tiles, too)
+    asm volatile("" ::: "memory");
   }
 
   f4 acc[NE + 1];
@@ -615,24 +676,19 @@ __global__ __launch_bounds__(256, 3) void kv4_attn_few_kernel(Kv4Pool p, Kv4Rows
   for (int e = 0; e <= NE; ++e) acc[e] = f4{0.f, 0.f, 0.f, 0.f};
   float m = -INFINITY;
 
-  // One tile's registers: the next tile's keys are requested as soon as the scores are there, its values as soon as this
-  // tile's are operands.
+  // Loads of a wave land in the order in which they were issued: keys and values of a tile, then those of the next.  A wait
+  // leaves what is younger than its half of a tile in flight, and a half is fetched anew once its reads have arrived.
   const Kv4Bits bits;
   Kv4Tile<HD> tile;
-  int t = t0 + wave;
-  u32x2 at{0, 0};
-  u32 has = 0;                                                             // keys of the tile that have a row
-  if (t < t1) {
-    const auto first = place(t, look(t), 0, has);
-    at = look(t + KV4_WAVES);
-    keys.load_keys(first, tile);
-    keys.load_values(first, tile);
-  }
-  for (int buf = 1; t < t1; t += KV4_WAVES, buf ^= 1) {
+  for (int slot = 0; t < t1; t += KV4_WAVES, slot ^= 1) {
     const int u0 = t * KV4_TILE;
-    u32 next_has;
-    const auto next = place(t + KV4_WAVES, at, buf, next_has);
-    at = look(t + 2 * KV4_WAVES);
+    u32 has2;
+    const auto where = place(t + 2 * KV4_WAVES, at, has2);
+    at = look(t + 3 * KV4_WAVES);
+    wait_vm_at_most<3 * Ring::LOADS>();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    ring.read_keys(slot, tile);
     if (NEW && pnew >= u0 && pnew < u0 + KV4_TILE) {
       const int n0 = pnew - u0;
       const u32x4 code = HD == 128 ? *reinterpret_cast<const u32x4*>(&s_new[0][h * (HD / 32)])
@@ -640,18 +696,16 @@ __global__ __launch_bounds__(256, 3) void kv4_attn_few_kernel(Kv4Pool p, Kv4Rows
       const u32 param = s_newp[0][HD == 128 ? h : h >> 1];
       if (n0 == c) { tile.k0 = code; tile.kp[0] = param; }
       if (n0 == 16 + c) { tile.k1 = code; tile.kp[1] = param; }
-      const u32 vcode = HD == 128 ? s_new[1][c] : (s_new[1][c >> 1] >> (16 * (c & 1))) & 0xffff;
-      const u32 vparam = s_newp[1][c * (HD / 16) / KV4_GROUP];
-#pragma unroll
-      for (int n = 0; n < 8; ++n)
-        if (n0 == kv4_key(n, h)) { tile.v[n] = vcode; tile.vp[n] = vparam; }
     }
+    wait_lgkm_at_most<0>();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    ring.fetch_keys(slot, where);
+    __builtin_amdgcn_sched_barrier(0);
     f4 s0, s1;
     kv4_scores<HD>(tile, query, bits, s0, s1);
     s0 *= query.scale;
     s1 *= query.scale;
-    __builtin_amdgcn_sched_barrier(0);
-    keys.load_keys(next, tile);
     if (u0 + KV4_TILE - 1 > first_limit || ~has) {                         // some query does not see some key
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -687,6 +741,24 @@ __global__ __launch_bounds__(256, 3) void kv4_attn_few_kernel(Kv4Pool p, Kv4Rows
       acc[e] = kv4_mfma(o, __builtin_bit_cast(h8, ph), acc[e]);
       if (TWO) acc[e] = kv4_mfma(o, __builtin_bit_cast(h8, pl), acc[e]);
     };
+    __builtin_amdgcn_sched_barrier(0);
+    wait_vm_at_most<3 * Ring::LOADS>();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    ring.read_values(slot, tile);
+    if (NEW && pnew >= u0 && pnew < u0 + KV4_TILE) {
+      const int n0 = pnew - u0;
+      const u32 code = HD == 128 ? s_new[1][c] : (s_new[1][c >> 1] >> (16 * (c & 1))) & 0xffff;
+      const u32 param = s_newp[1][c * (HD / 16) / KV4_GROUP];
+#pragma unroll
+      for (int n = 0; n < 8; ++n)
+        if (n0 == kv4_key(n, h)) { tile.v[n] = code; tile.vp[n] = param; }
+    }
+    wait_lgkm_at_most<0>();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    ring.fetch_values(slot, where);
+    __builtin_amdgcn_sched_barrier(0);
     add(NE, kv4_middles<HD>(tile, has, c, h));
     h8 op[4];
     kv4_values<HD, 0>(tile, bits, op);
@@ -694,41 +766,42 @@ __global__ __launch_bounds__(256, 3) void kv4_attn_few_kernel(Kv4Pool p, Kv4Rows
     for (int i = 0; i < 4; ++i) add(i, op[i]);
     if (HD == 128) {
       kv4_values<HD, 1>(tile, bits, op);
-      __builtin_amdgcn_sched_barrier(0);
-      keys.load_values(next, tile);
 #pragma unroll
       for (int i = 0; i < 4; ++i) add(4 * (HD / 128) + i, op[i]);
-    } else {
-      __builtin_amdgcn_sched_barrier(0);
-      keys.load_values(next, tile);
     }
-    has = next_has;
+    has = has1;
+    has1 = has2;
   }
+  wait_vm_at_most<0>();                                                    // the loads ahead must not land in what follows
 
   // the waves' softmaxes meet
   if (h == 0) s_m[wave][c] = m;
   __syncthreads();
+  typedef float Meet[NE + 1][64][4];
+  Meet* meet = reinterpret_cast<Meet*>(s_mem);
   float top = s_m[0][c];
 #pragma unroll
   for (int i = 1; i < KV4_WAVES; ++i) top = fmaxf(top, s_m[i][c]);
   const float weight = m > -INFINITY ? __builtin_amdgcn_exp2f(m - top) : 0.f;
 #pragma unroll
   for (int e = 0; e <= NE; ++e)
-    *reinterpret_cast<f4*>(s_mem.meet.acc[wave][e][lane]) = acc[e] * weight;
+    *reinterpret_cast<f4*>(meet[wave][e][lane]) = acc[e] * weight;
   __syncthreads();
   f4 sums[NE / KV4_WAVES], extra{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int n = 0; n < NE / KV4_WAVES; ++n) {
     sums[n] = f4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int i = 0; i < KV4_WAVES; ++i) sums[n] += *reinterpret_cast<const f4*>(s_mem.meet.acc[i][wave * (NE / KV4_WAVES) + n][lane]);
+    for (int i = 0; i < KV4_WAVES; ++i) sums[n] += *reinterpret_cast<const f4*>(meet[i][wave * (NE / KV4_WAVES) + n][lane]);
   }
 #pragma unroll
-  for (int i = 0; i < KV4_WAVES; ++i) extra += *reinterpret_cast<const f4*>(s_mem.meet.acc[i][NE][lane]);
+  for (int i = 0; i < KV4_WAVES; ++i) extra += *reinterpret_cast<const f4*>(meet[i][NE][lane]);
   float l = 0.f;
 #pragma unroll
-  for (int i = 0; i < KV4_WAVES; ++i) l += s_mem.meet.acc[i][NE][c][1];
+  for (int i = 0; i < KV4_WAVES; ++i) l += meet[i][NE][c][1];
   __syncthreads();
+  typedef float Out[HD + 4];
+  Out* out = reinterpret_cast<Out*>(s_mem);
   const float mid = extra[2] != 0.f ? NAN : extra[0];                      // a NaN mark with any weight
   const float inv = splits > 1 ? 1.0f : l != 0.f ? 1.0f / l : 0.f;
 #pragma unroll
@@ -736,7 +809,7 @@ __global__ __launch_bounds__(256, 3) void kv4_attn_few_kernel(Kv4Pool p, Kv4Rows
 #pragma unroll
     for (int i = 0; i < 4; ++i) {                                          // element (HD / 16) (4 h + i) + e
       const int e = (HD / 16) * (4 * h + i) + wave * (NE / KV4_WAVES) + n;
-      s_mem.out[c][e] = (sums[n][i] + mid) * inv;
+      out[c][e] = (sums[n][i] + mid) * inv;
     }
   __syncthreads();
   if (splits == 1) {
@@ -745,14 +818,14 @@ __global__ __launch_bounds__(256, 3) void kv4_attn_few_kernel(Kv4Pool p, Kv4Rows
       if (ff >= rows) break;
       u16x8 v;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = T::store(s_mem.out[row][oct * 8 + e]);
+      for (int e = 0; e < 8; ++e) v[e] = T::store(out[row][oct * 8 + e]);
       kv4_store8(o, s.first + jj, w.head * share_heads + ff - jj * share_heads, oct * 8, v);
     }
   } else {
     float* to = part + (size_t)blockIdx.x * 16 * (HD + 2);
     for (int i = tid; i < min(16, rows - f0) * (HD / 4); i += 256) {
       const int row = i / (HD / 4), x = i % (HD / 4);
-      *reinterpret_cast<f4*>(to + row * HD + x * 4) = *reinterpret_cast<const f4*>(&s_mem.out[row][x * 4]);
+      *reinterpret_cast<f4*>(to + row * HD + x * 4) = *reinterpret_cast<const f4*>(&out[row][x * 4]);
     }
     if (tid < 16) {
       to[16 * HD + tid] = top;
