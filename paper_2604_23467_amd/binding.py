@@ -266,6 +266,7 @@ class KV4Cache:
         if not pool.is_cuda or not pool.is_contiguous():
             raise ValueError("the pool must be a contiguous CUDA tensor")
         self.pool, self.n_kv_heads, self.head_dim = pool, n_kv_heads, head_dim
+        self.device, self.index = pool.device, pool.get_device()
         self.c = LLKV4Cache(pool.data_ptr(), pool.numel() * pool.element_size(), n_kv_heads, head_dim, page_tokens, n_pages)
 
 
@@ -275,66 +276,73 @@ class KV4Rows:
 
     def __init__(self, lens, page_table, max_rows=1, row_start=None, max_len=0):
         import torch
+        index = lens.get_device()
         for t in (lens, page_table) if row_start is None else (lens, page_table, row_start):
-            if t.dtype != torch.int32 or not t.is_contiguous() or t.device != lens.device or not t.is_cuda:
+            if t.dtype != torch.int32 or not t.is_contiguous() or not t.is_cuda or t.get_device() != index:
                 raise ValueError("lens, page_table and row_start must be contiguous int32 tensors of one CUDA device")
         n = lens.shape[0]
         if lens.dim() != 1 or page_table.dim() != 2 or page_table.shape[0] != n or \
                 (row_start is not None and row_start.shape != (n + 1,)):
             raise ValueError("lens [n_seqs], page_table [n_seqs, pages] and row_start [n_seqs + 1] do not fit together")
-        self.lens, self.page_table, self.row_start = lens, page_table, row_start
+        self.lens, self.page_table, self.row_start, self.index = lens, page_table, row_start, index
         self.c = LLKV4Rows(None if row_start is None else row_start.data_ptr(), lens.data_ptr(), page_table.data_ptr(),
                            n, max_rows, 0, page_table.shape[1], max_len)
 
 
-def _kv4_view(t, name, cache, heads, like=None):
-    if t.dim() != 3 or t.shape[2] != cache.head_dim or (heads and t.shape[1] != heads):
-        raise ValueError("%s must be [rows, %s, %d]" % (name, heads or "heads", cache.head_dim))
-    if like is not None and (t.dtype != like.dtype or t.shape[0] != like.shape[0]):
-        raise ValueError("%s must have the other tensors' type and rows" % name)
-    if t.device != cache.pool.device or t.stride(2) != 1:
-        raise ValueError("%s must be on the pool's device with a contiguous last dimension" % name)
-    return LLKV4View(t.data_ptr(), t.stride(0), t.stride(1))
+def _kv4_view(t, name, cache, heads, n_rows, dtype):
+    shape, strides = t.shape, t.stride()
+    if len(shape) != 3 or shape[0] != n_rows or shape[1] != heads or shape[2] != cache.head_dim:
+        raise ValueError("%s must be [%d, %d, %d], is %s" % (name, n_rows, heads, cache.head_dim, list(shape)))
+    if t.dtype is not dtype or strides[2] != 1 or t.get_device() != cache.index:
+        raise ValueError("%s must be a %s tensor on the pool's device with a contiguous last dimension" % (name, dtype))
+    return LLKV4View(t.data_ptr(), strides[0], strides[1])
 
 
-def _kv4_type(t):
+def _kv4_type(dtype):
     import torch
-    if t.dtype not in (torch.float16, torch.bfloat16):
-        raise ValueError("rows are float16 or bfloat16, not %s" % t.dtype)
-    return LL_F16 if t.dtype == torch.float16 else LL_BF16
+    if dtype is torch.float16:
+        return LL_F16
+    if dtype is torch.bfloat16:
+        return LL_BF16
+    raise ValueError("rows are float16 or bfloat16, not %s" % dtype)
 
 
-def _kv4_on(cache, rows, stream):
-    """A context with the stream to work on (None: the current one of the pool's device) and its device as torch's current
-    ones, so that what the call allocates belongs to them, and the stream's handle."""
+def _kv4_do(cache, rows, n_rows, stream, call):
+    """call(stream handle) with the pool's device as the current one, and, where ``stream`` is given instead of torch's current
+    one, with it as the current stream, so that what the call allocates belongs to it."""
     import torch
-    if rows.lens.device != cache.pool.device:
+    if rows.index != cache.index:
         raise ValueError("lens and page_table must be on the pool's device")
-    if stream is None:
-        stream = torch.cuda.current_stream(cache.pool.device)
-    return torch.cuda.stream(stream), C.c_void_p(stream.cuda_stream)
+    rows.c.n_rows = n_rows
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return call(stream.cuda_stream)
+    if torch._C._cuda_getDevice() != cache.index:
+        with torch.cuda.device(cache.index):
+            return call(torch._C._cuda_getCurrentRawStream(cache.index))
+    return call(torch._C._cuda_getCurrentRawStream(cache.index))
 
 
 def ll_kv4_write(cache, rows, k, v, stream=None):
     """Quantises rows of k and v, [rows, n_kv_heads, head_dim] float16 or bfloat16, into the cache."""
-    kv, vv = _kv4_view(k, "k", cache, cache.n_kv_heads), _kv4_view(v, "v", cache, cache.n_kv_heads, k)
-    rows.c.n_rows = k.shape[0]
-    on, s = _kv4_on(cache, rows, stream)
-    with on:
-        _check(load().ll_kv4_write(C.byref(cache.c), C.byref(rows.c), _kv4_type(k), C.byref(kv), C.byref(vv), s))
+    n, dtype = k.shape[0], k.dtype
+    kind, kv, vv = _kv4_type(dtype), _kv4_view(k, "k", cache, cache.n_kv_heads, n, dtype), _kv4_view(v, "v", cache, cache.n_kv_heads, n, dtype)
+    _kv4_do(cache, rows, n, stream, lambda s: _check(load().ll_kv4_write(C.byref(cache.c), C.byref(rows.c), kind, C.byref(kv), C.byref(vv), s)))
 
 
 def ll_kv4_read(cache, rows, k=None, v=None, n_rows=0, dtype=None, stream=None):
     """The rows out of the cache into k and v, or into new tensors of n_rows rows."""
     import torch
-    on, s = _kv4_on(cache, rows, stream)
-    with on:
-        if k is None:
-            k, v = torch.empty(2, n_rows, cache.n_kv_heads, cache.head_dim, dtype=dtype, device=cache.pool.device)
-        kv, vv = _kv4_view(k, "k", cache, cache.n_kv_heads), _kv4_view(v, "v", cache, cache.n_kv_heads, k)
-        rows.c.n_rows = k.shape[0]
-        _check(load().ll_kv4_read(C.byref(cache.c), C.byref(rows.c), _kv4_type(k), C.byref(kv), C.byref(vv), s))
-    return k, v
+    if k is not None:
+        n_rows, dtype = k.shape[0], k.dtype
+    kind = _kv4_type(dtype)
+
+    def call(s):
+        a, b = (k, v) if k is not None else torch.empty((2, n_rows, cache.n_kv_heads, cache.head_dim), dtype=dtype, device=cache.device)
+        kv, vv = _kv4_view(a, "k", cache, cache.n_kv_heads, n_rows, dtype), _kv4_view(b, "v", cache, cache.n_kv_heads, n_rows, dtype)
+        _check(load().ll_kv4_read(C.byref(cache.c), C.byref(rows.c), kind, C.byref(kv), C.byref(vv), s))
+        return a, b
+    return _kv4_do(cache, rows, n_rows, stream, call)
 
 
 def ll_kv4_attention_workspace_bytes(cache, rows, n_heads, n_rows):
@@ -347,24 +355,30 @@ def ll_kv4_attention(cache, rows, q, k=None, v=None, scale=0.0, out=None, worksp
     """Causal attention of rows q [rows, heads, head_dim] over the cache; k and v: these rows' own, written first.
     Without ``workspace`` (a CUDA tensor on a 256-byte border) the call takes one from torch's allocator where it needs any."""
     import torch
-    qv = _kv4_view(q, "q", cache, 0)
-    kv = None if k is None else C.byref(_kv4_view(k, "k", cache, cache.n_kv_heads, None))
-    vv = None if v is None else C.byref(_kv4_view(v, "v", cache, cache.n_kv_heads, None))
-    for t in (k, v, out):
-        if t is not None and (t.dtype != q.dtype or t.shape[0] != q.shape[0]):
-            raise ValueError("q, k, v and out must have the same type and number of rows")
-    on, s = _kv4_on(cache, rows, stream)
-    with on:
-        if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        nbytes = ll_kv4_attention_workspace_bytes(cache, rows, q.shape[1], q.shape[0])
-        if workspace is None and nbytes:
-            workspace = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
-        _check(load().ll_kv4_attention(C.byref(cache.c), C.byref(rows.c), _kv4_type(q), q.shape[1], scale, C.byref(qv), kv, vv,
-                                       C.byref(_kv4_view(out, "out", cache, q.shape[1])),
-                                       None if workspace is None else C.c_void_p(workspace.data_ptr()),
-                                       0 if workspace is None else workspace.numel() * workspace.element_size(), s))
-    return out
+    shape, dtype = q.shape, q.dtype
+    if len(shape) != 3:
+        raise ValueError("q must be [rows, heads, %d]" % cache.head_dim)
+    n, heads = shape[0], shape[1]
+    kind, qv = _kv4_type(dtype), _kv4_view(q, "q", cache, heads, n, dtype)
+    kv = None if k is None else C.byref(_kv4_view(k, "k", cache, cache.n_kv_heads, n, dtype))
+    vv = None if v is None else C.byref(_kv4_view(v, "v", cache, cache.n_kv_heads, n, dtype))
+
+    def call(s):
+        o = torch.empty(shape, dtype=dtype, device=cache.device) if out is None else out
+        ov = _kv4_view(o, "out", cache, heads, n, dtype)
+        w, nbytes = workspace, 0
+        if w is None:
+            nbytes = ll_kv4_attention_workspace_bytes(cache, rows, heads, n)
+            if nbytes:
+                w = torch.empty(nbytes, dtype=torch.uint8, device=cache.device)
+        else:
+            if w.get_device() != cache.index or not w.is_contiguous():
+                raise ValueError("workspace must be a contiguous tensor on the pool's device")
+            nbytes = w.numel() * w.element_size()
+        _check(load().ll_kv4_attention(C.byref(cache.c), C.byref(rows.c), kind, heads, scale, C.byref(qv), kv, vv, C.byref(ov),
+                                       w.data_ptr() if nbytes else None, nbytes, s))
+        return o
+    return _kv4_do(cache, rows, n, stream, call)
 
 
 class Session:
