@@ -84,10 +84,20 @@ void kv4_dispatch(int32_t dtype, int head_dim, F&& go) {
   else head_dim == 128 ? go(Kv4Bf16{}, Kv4Dim<128>{}) : go(Kv4Bf16{}, Kv4Dim<64>{});
 }
 
+// Blocks of 8 rows where that leaves every CU with work of several workgroups; single rows, whose chain is shorter, else
+constexpr int kKv4RowBlock = 8;
+template <class F>
+void kv4_row_blocks(const Kv4Pool& p, const Kv4Rows& r, int head_dim, F&& go) {
+  const int parts = (2 * p.kv_heads * (head_dim / 8) + 255) / 256;
+  if ((int64_t)r.n_rows * parts >= (int64_t)2 * kKv4RowBlock * num_cus()) go(Kv4Dim<kKv4RowBlock>{}, dim3((r.n_rows + kKv4RowBlock - 1) / kKv4RowBlock, parts));
+  else go(Kv4Dim<1>{}, dim3(r.n_rows, parts));
+}
+
 void kv4_launch_write(hipStream_t s, int32_t dtype, int head_dim, const Kv4Pool& p, const Kv4Rows& r, const Kv4View& k, const Kv4View& v) {
-  const dim3 grid(r.n_rows, (2 * p.kv_heads * (head_dim / 8) + 255) / 256);
   kv4_dispatch(dtype, head_dim, [&](auto t, auto hd) {
-    hipLaunchKernelGGL((kv4_write_kernel<decltype(t), decltype(hd)::value>), grid, dim3(256), 0, s, p, r, k, v);
+    kv4_row_blocks(p, r, head_dim, [&](auto n, dim3 grid) {
+      hipLaunchKernelGGL((kv4_write_kernel<decltype(t), decltype(hd)::value, decltype(n)::value>), grid, dim3(256), 0, s, p, r, k, v);
+    });
   });
 }
 
@@ -165,10 +175,11 @@ int ll_kv4_read(const ll_kv4_cache* cache, const ll_kv4_rows* rows, int32_t dtyp
   if (r.n_seqs == 0 || r.n_rows == 0) return LL_OK;
   if ((rc = kv4_check_view(who, "k", k, rows, p.kv_heads, cache->head_dim, true, &kk)) != LL_OK ||
       (rc = kv4_check_view(who, "v", v, rows, p.kv_heads, cache->head_dim, true, &vv)) != LL_OK) return rc;
-  const dim3 grid(r.n_rows, (2 * p.kv_heads * (cache->head_dim / 8) + 255) / 256);
   kv4_dispatch(dtype, cache->head_dim, [&](auto t, auto hd) {
-    hipLaunchKernelGGL((kv4_read_kernel<decltype(t), decltype(hd)::value>), grid, dim3(256), 0, static_cast<hipStream_t>(hip_stream),
-                       p, r, kk, vv);
+    kv4_row_blocks(p, r, cache->head_dim, [&](auto n, dim3 grid) {
+      hipLaunchKernelGGL((kv4_read_kernel<decltype(t), decltype(hd)::value, decltype(n)::value>), grid, dim3(256), 0,
+                         static_cast<hipStream_t>(hip_stream), p, r, kk, vv);
+    });
   });
   HIPCHK(hipGetLastError());
   return LL_OK;

@@ -80,16 +80,24 @@ __device__ __forceinline__ Kv4Seq kv4_seq(const Kv4Rows& r, int b) {
   return s;
 }
 
-// Sequence of row i, or -1: all 64 lanes of a wave look at a sequence each
-__device__ __forceinline__ int kv4_find(const Kv4Rows& r, int i) {
-  if (!r.row_start) return i / r.max_rows;
+// Sequences of the rows from i0 on, -1 where a row has none: all 64 lanes of a wave look at a sequence each
+template <int N>
+__device__ __forceinline__ void kv4_find(const Kv4Rows& r, int i0, int (&b)[N]) {
+#pragma unroll
+  for (int n = 0; n < N; ++n) b[n] = r.row_start || i0 + n >= r.n_rows ? -1 : (i0 + n) / r.max_rows;
+  if (!r.row_start) return;
   const int lane = threadIdx.x & 63;
   for (int b0 = 0; b0 < r.n_seqs; b0 += 64) {
-    const int b = min(b0 + lane, r.n_seqs - 1);
-    const unsigned long long hit = __ballot(i >= r.row_start[b] && i < r.row_start[b + 1]);
-    if (hit) return b0 + __ffsll(hit) - 1;
+    const int mine = min(b0 + lane, r.n_seqs - 1), from = r.row_start[mine], to = min(r.row_start[mine + 1], r.n_rows);
+    int missing = 0;
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const unsigned long long hit = __ballot(i0 + n >= from && i0 + n < to);
+      if (b[n] < 0 && hit) b[n] = b0 + __ffsll(hit) - 1;
+      missing |= b[n] < 0;
+    }
+    if (!missing) return;
   }
-  return -1;
 }
 
 // Pool row of position u >= 0 of the sequence with this page-table row; -1 where there is none
@@ -98,6 +106,26 @@ __device__ __forceinline__ int kv4_row(const Kv4Pool& p, const int* table, int t
   if (page >= table_stride) return -1;
   const int at = table[page];
   return (u32)at <= (u32)(p.pool_rows - p.page_tokens) ? at + (u - page * p.page_tokens) : -1;
+}
+
+// Pool rows of the call's rows from i0 on: -1 where a row's position has none, -2 where the row is none of the call's
+template <int N>
+__device__ __forceinline__ void kv4_places(const Kv4Pool& p, const Kv4Rows& r, int i0, int (&row)[N]) {
+  int b[N];
+  kv4_find<N>(r, i0, b);
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    row[n] = -2;
+    if (b[n] < 0) continue;
+    const Kv4Seq s = kv4_seq(r, b[n]);
+    const int j = i0 + n - s.first, pos = s.len - s.rows + j;
+    if (j >= r.max_rows) continue;
+    row[n] = -1;
+    const int page = (int)(__umulhi((u32)pos << 1, p.magic) >> p.shift);
+    if (pos < 0 || page >= r.table_stride) continue;
+    const int at = kv4_scalar(r.table + (size_t)b[n] * r.table_stride + page);
+    if ((u32)at <= (u32)(p.pool_rows - p.page_tokens)) row[n] = at + (pos - page * p.page_tokens);
+  }
 }
 
 // ---- element types at the borders: binary16 and bfloat16 ----
@@ -149,108 +177,113 @@ __device__ __forceinline__ float kv4_quad_max(float v) { return fmaxf(v, dpp_mov
 
 // Four neighbouring lanes hold a group, 8 elements each: the lane's 8 codes (element i in bits 4 i ..) and the group's
 // parameters (s in the low half).  What a float cannot decide is decided in 64 bits: whether 15 s reaches the span, and the
-// code of an element closer than the float's error to the border between two (some 1e-5 of them).
+// code of an element closer than the float's error (three roundings of a number below 16) to the border between two.
 __device__ __forceinline__ u32 kv4_quantise(const float (&x)[8], u32& param) {
-  float lo = x[0], hi = x[0];
-  bool bad = false;
+  float lo = fminf(x[0], x[1]), hi = fmaxf(x[0], x[1]);
+  float zero = x[0] * 0.f;                             // NaN if an element is NaN or infinite
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
+  for (int i = 1; i < 8; ++i) {
     lo = fminf(lo, x[i]);
     hi = fmaxf(hi, x[i]);
-    bad |= !(fabsf(x[i]) < INFINITY);
+    zero = fmaf(x[i], 0.f, zero);
   }
   lo = kv4_quad_min<0x4E>(kv4_quad_min<0xB1>(lo));
   hi = kv4_quad_max<0x4E>(kv4_quad_max<0xB1>(hi));
+  zero += dpp_mov<0xB1>(zero);
+  zero += dpp_mov<0x4E>(zero);
   const double span = (double)hi - (double)lo;
-  float s = 0.f;
-  if (hi > lo) {
-    s = kv4_step_up((hi - lo) * (1.0f / 15.0f));
-    if (15.0 * (double)s < span) s = kv4_step_next(s, 1);
-    const float below = kv4_step_next(s, -1);
-    if (15.0 * (double)below >= span) s = below;
-  }
+  float s = kv4_step_up((hi - lo) * (1.0f / 15.0f));
+  if (15.0 * (double)s < span) s = kv4_step_next(s, 1);
+  const float below = kv4_step_next(s, -1);
+  if (s > 0.f && 15.0 * (double)below >= span) s = below;
   const half_t mid_h = (half_t)(float)((double)lo + 8.0 * (double)s);
-  float mid = (float)mid_h;
-  float flag = bad || !(s <= KV4_MAX_STEP) || !(fabsf(mid) < INFINITY) ? 1.f : 0.f;
-  flag = kv4_quad_max<0x4E>(kv4_quad_max<0xB1>(flag));
-  if (flag != 0.f) {
+  const float mid = (float)mid_h;
+  if (!(zero == 0.f) || !(s <= KV4_MAX_STEP) || !(fabsf(mid) < INFINITY)) {
     param = 0x7e007e00u;
     return 0;
   }
   param = (u32)__builtin_bit_cast(u16, (half_t)s) | (u32)__builtin_bit_cast(u16, mid_h) << 16;
   const float inv = s > 0.f ? 1.0f / s : 0.f;
-  int c[8];
-  bool near = false;
+  float c[8], off = 0.f;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const float y = (x[i] - mid) * inv, n = rintf(y);
-    near |= fabsf(fabsf(y - n) - 0.5f) < 1e-5f;
-    c[i] = (int)fminf(fmaxf(n, -8.f), 7.f) + 8;
+    off = fmaxf(off, fabsf(y - n));
+    c[i] = __builtin_amdgcn_fmed3f(n, -8.f, 7.f);
   }
-  if (__any(near) && s > 0.f) {
+  if (__any(off > 0.49999f)) {
+    if (s > 0.f) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const double n = rint(((double)x[i] - (double)mid) / (double)s);
-      c[i] = (int)fmin(fmax(n, -8.0), 7.0) + 8;
+      for (int i = 0; i < 8; ++i)
+        c[i] = __builtin_amdgcn_fmed3f((float)rint(((double)x[i] - (double)mid) / (double)s), -8.f, 7.f);
     }
   }
-  u32 w = 0;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) w |= (u32)c[i] << (4 * i);
-  return w;
+  auto four = [](float a, float b, float d, float e) {   // c + 8 of four elements in 16 bits: whole numbers, exact
+    return (u32)fmaf(fmaf(e, 16.f, d), 256.f, fmaf(b, 16.f, a + 34952.f));
+  };
+  return four(c[0], c[1], c[2], c[3]) | four(c[4], c[5], c[6], c[7]) << 16;
 }
 
-// Rows of k and v into the cache.  A thread takes 8 elements, four threads a group.  grid = (rows, parts of a row's
-// 2 kv_heads HD / 8 threads).
-template <class T, int HD>
+// Rows of k and v into the cache.  A thread takes 8 elements of N consecutive rows, four threads a group.  grid = (blocks of N
+// rows, parts of a row's 2 kv_heads HD / 8 threads).  The cache has a head's rows side by side, so the rows of a block share
+// lines of it: written one by one from different XCDs, a line of parameters (8 rows) would leave eight L2s in parts.
+template <class T, int HD, int N>
 __global__ __launch_bounds__(256) void kv4_write_kernel(Kv4Pool p, Kv4Rows r, Kv4View k, Kv4View v) {
   constexpr int UPR = HD / 8;
-  const int b = kv4_find(r, blockIdx.x);
-  if (b < 0) return;
-  const Kv4Seq s = kv4_seq(r, b);
-  const int j = blockIdx.x - s.first, pos = s.len - s.rows + j;
-  if (j >= r.max_rows || pos < 0) return;
-  const int row = kv4_row(p, r.table + (size_t)b * r.table_stride, r.table_stride, pos);
-  if (row < 0) return;
-  const int units = p.kv_heads * UPR, t = blockIdx.y * 256 + threadIdx.x;
-  if (t >= 2 * units) return;
+  const int i0 = blockIdx.x * N, units = p.kv_heads * UPR, t = blockIdx.y * 256 + threadIdx.x;
   const int which = t >= units, unit = which ? t - units : t, head = unit / UPR, oct = unit % UPR;
-  const u16x8 in = kv4_load8(which ? v : k, s.first + j, head, oct * 8);
-  float x[8];
+  int row[N];
+  kv4_places<N>(p, r, i0, row);
+  if (t >= 2 * units) return;
+  const Kv4View from = which ? v : k;
+  u16x8 in[N];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] = T::load(in[i]);
-  u32 param;
-  const u32 w = kv4_quantise(x, param);
-  *(u32*)(kv4_codes<HD>(p, which, head) + (size_t)row * (HD / 2) + oct * 4) = w;
-  if (oct % 4 == 0) *(u32*)(kv4_params<HD>(p, which, head) + (size_t)row * (HD / 8) + oct) = param;
+  for (int n = 0; n < N; ++n)
+    if (row[n] >= 0) in[n] = kv4_load8(from, i0 + n, head, oct * 8);
+  char *codes = kv4_codes<HD>(p, which, head) + oct * 4, *params = kv4_params<HD>(p, which, head) + oct;
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    if (row[n] < 0) continue;
+    float x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = T::load(in[n][i]);
+    u32 param;
+    const u32 w = kv4_quantise(x, param);
+    *as_global(reinterpret_cast<u32*>(codes + (size_t)row[n] * (HD / 2))) = w;
+    if (oct % 4 == 0) *as_global(reinterpret_cast<u32*>(params + (size_t)row[n] * (HD / 8))) = param;
+  }
 }
 
 __device__ __forceinline__ float kv4_value(u32 w, int i, float s, float mid) {
   return fmaf(s, (float)((w >> (4 * i)) & 15) - 8.0f, mid);
 }
 
-// The same rows out of the cache.  Rows of positions that are not there are zeros; grid as kv4_write_kernel's.
-template <class T, int HD>
+// The same rows out of the cache.  Rows of positions that are not there are zeros; grid and blocks as kv4_write_kernel's.
+template <class T, int HD, int N>
 __global__ __launch_bounds__(256) void kv4_read_kernel(Kv4Pool p, Kv4Rows r, Kv4View k, Kv4View v) {
   constexpr int UPR = HD / 8;
-  const int b = kv4_find(r, blockIdx.x);
-  if (b < 0) return;
-  const Kv4Seq s = kv4_seq(r, b);
-  const int j = blockIdx.x - s.first, pos = s.len - s.rows + j;
-  if (j >= r.max_rows) return;
-  const int row = pos < 0 ? -1 : kv4_row(p, r.table + (size_t)b * r.table_stride, r.table_stride, pos);
-  const int units = p.kv_heads * UPR, t = blockIdx.y * 256 + threadIdx.x;
-  if (t >= 2 * units) return;
+  const int i0 = blockIdx.x * N, units = p.kv_heads * UPR, t = blockIdx.y * 256 + threadIdx.x;
   const int which = t >= units, unit = which ? t - units : t, head = unit / UPR, oct = unit % UPR;
-  u16x8 out{};
-  if (row >= 0) {
-    const u32 w = *(const u32*)(kv4_codes<HD>(p, which, head) + (size_t)row * (HD / 2) + oct * 4);
-    const u32 param = *(const u32*)(kv4_params<HD>(p, which, head) + (size_t)row * (HD / 8) + oct / 4 * 4);
-    const float sc = Kv4F16::load(param & 0xffff), mid = Kv4F16::load(param >> 16);
+  int row[N];
+  kv4_places<N>(p, r, i0, row);
+  if (t >= 2 * units) return;
+  const Kv4View to = which ? v : k;
+  const char *codes = kv4_codes<HD>(p, which, head) + oct * 4, *params = kv4_params<HD>(p, which, head) + oct / 4 * 4;
+  u32 w[N], param[N];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) out[i] = T::store(kv4_value(w, i, sc, mid));
+  for (int n = 0; n < N; ++n) {
+    w[n] = *as_global(reinterpret_cast<const u32*>(codes + (size_t)max(row[n], 0) * (HD / 2)));
+    param[n] = *as_global(reinterpret_cast<const u32*>(params + (size_t)max(row[n], 0) * (HD / 8)));
   }
-  kv4_store8(which ? v : k, s.first + j, head, oct * 8, out);
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    if (row[n] == -2) continue;
+    const float sc = Kv4F16::load(param[n] & 0xffff), mid = Kv4F16::load(param[n] >> 16);
+    u16x8 out;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) out[i] = row[n] < 0 ? (u16)0 : T::store(kv4_value(w[n], i, sc, mid));
+    kv4_store8(to, i0 + n, head, oct * 8, out);
+  }
 }
 
 // ---- attention ----
