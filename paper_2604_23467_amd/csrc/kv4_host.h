@@ -88,15 +88,16 @@ void kv4_dispatch(int32_t dtype, int head_dim, F&& go) {
 constexpr int kKv4RowBlock = 8;
 template <class F>
 void kv4_row_blocks(const Kv4Pool& p, const Kv4Rows& r, int head_dim, F&& go) {
-  const int parts = (2 * p.kv_heads * (head_dim / 8) + 255) / 256;
-  if ((int64_t)r.n_rows * parts >= (int64_t)2 * kKv4RowBlock * num_cus()) go(Kv4Dim<kKv4RowBlock>{}, dim3((r.n_rows + kKv4RowBlock - 1) / kKv4RowBlock, parts));
-  else go(Kv4Dim<1>{}, dim3(r.n_rows, parts));
+  const int units = p.kv_heads * (head_dim / 8), threads = std::min(256, (units + 63) / 64 * 64), parts = (units + threads - 1) / threads;
+  if ((int64_t)r.n_rows * parts * 2 >= (int64_t)2 * kKv4RowBlock * num_cus())
+    go(Kv4Dim<kKv4RowBlock>{}, dim3((r.n_rows + kKv4RowBlock - 1) / kKv4RowBlock, parts, 2), dim3(threads));
+  else go(Kv4Dim<1>{}, dim3(r.n_rows, parts, 2), dim3(threads));
 }
 
 void kv4_launch_write(hipStream_t s, int32_t dtype, int head_dim, const Kv4Pool& p, const Kv4Rows& r, const Kv4View& k, const Kv4View& v) {
   kv4_dispatch(dtype, head_dim, [&](auto t, auto hd) {
-    kv4_row_blocks(p, r, head_dim, [&](auto n, dim3 grid) {
-      hipLaunchKernelGGL((kv4_write_kernel<decltype(t), decltype(hd)::value, decltype(n)::value>), grid, dim3(256), 0, s, p, r, k, v);
+    kv4_row_blocks(p, r, head_dim, [&](auto n, dim3 grid, dim3 threads) {
+      hipLaunchKernelGGL((kv4_write_kernel<decltype(t), decltype(hd)::value, decltype(n)::value>), grid, threads, 0, s, p, r, k, v);
     });
   });
 }
@@ -176,8 +177,8 @@ int ll_kv4_read(const ll_kv4_cache* cache, const ll_kv4_rows* rows, int32_t dtyp
   if ((rc = kv4_check_view(who, "k", k, rows, p.kv_heads, cache->head_dim, true, &kk)) != LL_OK ||
       (rc = kv4_check_view(who, "v", v, rows, p.kv_heads, cache->head_dim, true, &vv)) != LL_OK) return rc;
   kv4_dispatch(dtype, cache->head_dim, [&](auto t, auto hd) {
-    kv4_row_blocks(p, r, cache->head_dim, [&](auto n, dim3 grid) {
-      hipLaunchKernelGGL((kv4_read_kernel<decltype(t), decltype(hd)::value, decltype(n)::value>), grid, dim3(256), 0,
+    kv4_row_blocks(p, r, cache->head_dim, [&](auto n, dim3 grid, dim3 threads) {
+      hipLaunchKernelGGL((kv4_read_kernel<decltype(t), decltype(hd)::value, decltype(n)::value>), grid, threads, 0,
                          static_cast<hipStream_t>(hip_stream), p, r, kk, vv);
     });
   });

@@ -108,24 +108,30 @@ __device__ __forceinline__ int kv4_row(const Kv4Pool& p, const int* table, int t
   return (u32)at <= (u32)(p.pool_rows - p.page_tokens) ? at + (u - page * p.page_tokens) : -1;
 }
 
-// Pool rows of the call's rows from i0 on: -1 where a row's position has none, -2 where the row is none of the call's
+// Pool rows of the call's rows from i0 on: -1 where a row's position has none, -2 where the row is none of the call's.  A lane
+// looks after a row: with scalar registers alone the rows would be worked out one after the other, in as many instructions as
+// quantising them takes.
 template <int N>
 __device__ __forceinline__ void kv4_places(const Kv4Pool& p, const Kv4Rows& r, int i0, int (&row)[N]) {
   int b[N];
   kv4_find<N>(r, i0, b);
+  const int i = threadIdx.x & (N - 1);
+  int mine = b[0];
 #pragma unroll
-  for (int n = 0; n < N; ++n) {
-    row[n] = -2;
-    if (b[n] < 0) continue;
-    const Kv4Seq s = kv4_seq(r, b[n]);
-    const int j = i0 + n - s.first, pos = s.len - s.rows + j;
-    if (j >= r.max_rows) continue;
-    row[n] = -1;
-    const int page = (int)(__umulhi((u32)pos << 1, p.magic) >> p.shift);
-    if (pos < 0 || page >= r.table_stride) continue;
-    const int at = kv4_scalar(r.table + (size_t)b[n] * r.table_stride + page);
-    if ((u32)at <= (u32)(p.pool_rows - p.page_tokens)) row[n] = at + (pos - page * p.page_tokens);
+  for (int n = 1; n < N; ++n) mine = i == n ? b[n] : mine;
+  const int at = max(mine, 0), len = max(r.len[at], 0) + r.len_add;
+  int first = at * r.max_rows, rows = r.max_rows;
+  if (r.row_start) {
+    first = min(max(r.row_start[at], 0), r.n_rows);
+    rows = min(max(r.row_start[at + 1], first), r.n_rows) - first;
   }
+  const int j = i0 + i - first, pos = (r.active && !r.active[at] ? 0 : len) - rows + j;
+  const int page = (int)(__umulhi((u32)max(pos, 0) << 1, p.magic) >> p.shift);
+  const int entry = r.table[(size_t)at * r.table_stride + min(page, r.table_stride - 1)];
+  const bool ok = pos >= 0 && page < r.table_stride && (u32)entry <= (u32)(p.pool_rows - p.page_tokens);
+  const int found = mine < 0 || j >= r.max_rows ? -2 : ok ? entry + (pos - page * p.page_tokens) : -1;
+#pragma unroll
+  for (int n = 0; n < N; ++n) row[n] = __builtin_amdgcn_readlane(found, n);
 }
 
 // ---- element types at the borders: binary16 and bfloat16 ----
@@ -143,7 +149,7 @@ struct Kv4Bf16 {
   }
 };
 __device__ __forceinline__ u16x8 kv4_load8(const Kv4View& t, int row, int head, int e) {
-  const u16* p = (const u16*)t.data + row * t.row_stride + head * t.head_stride + e;
+  const u16* p = (const u16*)t.data + row * t.row_stride + (head * t.head_stride + e);
   if (t.wide) return *as_global(reinterpret_cast<const u16x8*>(p));
   u16x8 v;
 #pragma unroll
@@ -151,7 +157,7 @@ __device__ __forceinline__ u16x8 kv4_load8(const Kv4View& t, int row, int head, 
   return v;
 }
 __device__ __forceinline__ void kv4_store8(const Kv4View& t, int row, int head, int e, u16x8 v) {
-  u16* p = (u16*)t.data + row * t.row_stride + head * t.head_stride + e;
+  u16* p = (u16*)t.data + row * t.row_stride + (head * t.head_stride + e);
   if (t.wide) {
     *as_global(reinterpret_cast<u16x8*>(p)) = v;
   } else {
@@ -162,8 +168,9 @@ __device__ __forceinline__ void kv4_store8(const Kv4View& t, int row, int head, 
 
 // A number that is a binary16 number of at most 8 significant bits: rounded up to the next one (x >= 0)
 __device__ __forceinline__ float kv4_step_up(float x) {
-  if (x < 0x1p-16f) return ceilf(x * 0x1p24f) * 0x1p-24f;          // binary16's smallest step
-  return __builtin_bit_cast(float, (__builtin_bit_cast(u32, x) + 0xffff) & 0xffff0000u);
+  const float few = ceilf(x * 0x1p24f) * 0x1p-24f;                 // below, binary16's smallest step is the coarser one
+  const float many = __builtin_bit_cast(float, (__builtin_bit_cast(u32, x) + 0xffff) & 0xffff0000u);
+  return x < 0x1p-16f ? few : many;
 }
 __device__ __forceinline__ float kv4_step_next(float s, int dir) {   // s > 0: its neighbour of that kind
   if (s < 0x1p-16f || (s == 0x1p-16f && dir < 0)) return s + dir * 0x1p-24f;
@@ -176,46 +183,54 @@ template <int CTRL>
 __device__ __forceinline__ float kv4_quad_max(float v) { return fmaxf(v, dpp_mov<CTRL>(v)); }
 
 // Four neighbouring lanes hold a group, 8 elements each: the lane's 8 codes (element i in bits 4 i ..) and the group's
-// parameters (s in the low half).  What a float cannot decide is decided in 64 bits: whether 15 s reaches the span, and the
-// code of an element closer than the float's error (three roundings of a number below 16) to the border between two.
+// parameters (s in the low half).  Whether 15 s reaches the span is decided in 64 bits.  A code is the nearest whole number to
+// the correctly rounded quotient (x - mid) / s, which is halfway between two whole numbers only where the exact one is, as long
+// as x and mid are multiples of s / 2^20 and x - mid is exact: true but for numbers 2^9 times smaller than s.  Where there are
+// such and an element lies near a border, 64 bits decide.
 __device__ __forceinline__ u32 kv4_quantise(const float (&x)[8], u32& param) {
   float lo = fminf(x[0], x[1]), hi = fmaxf(x[0], x[1]);
-  float zero = x[0] * 0.f;                             // NaN if an element is NaN or infinite
+  bool nan = __builtin_isunordered(x[0], x[1]);        // (an infinity shows in the span)
 #pragma unroll
-  for (int i = 1; i < 8; ++i) {
-    lo = fminf(lo, x[i]);
-    hi = fmaxf(hi, x[i]);
-    zero = fmaf(x[i], 0.f, zero);
+  for (int i = 2; i < 8; i += 2) {
+    lo = fminf(lo, fminf(x[i], x[i + 1]));
+    hi = fmaxf(hi, fmaxf(x[i], x[i + 1]));
+    nan |= __builtin_isunordered(x[i], x[i + 1]);
   }
   lo = kv4_quad_min<0x4E>(kv4_quad_min<0xB1>(lo));
   hi = kv4_quad_max<0x4E>(kv4_quad_max<0xB1>(hi));
-  zero += dpp_mov<0xB1>(zero);
-  zero += dpp_mov<0x4E>(zero);
+  const unsigned long long nans = __ballot(nan);
   const double span = (double)hi - (double)lo;
   float s = kv4_step_up((hi - lo) * (1.0f / 15.0f));
   if (15.0 * (double)s < span) s = kv4_step_next(s, 1);
   const float below = kv4_step_next(s, -1);
   if (s > 0.f && 15.0 * (double)below >= span) s = below;
-  const half_t mid_h = (half_t)(float)((double)lo + 8.0 * (double)s);
+  const half_t mid_h = (half_t)sk_fp32((float)fma(8.0, (double)s, (double)lo));      // by way of 32 bits, in two instructions
   const float mid = (float)mid_h;
-  if (!(zero == 0.f) || !(s <= KV4_MAX_STEP) || !(fabsf(mid) < INFINITY)) {
+  if ((nans && (nans >> (threadIdx.x & 60) & 15)) || !(s <= KV4_MAX_STEP) || !(fabsf(mid) < INFINITY)) {
     param = 0x7e007e00u;
     return 0;
   }
   param = (u32)__builtin_bit_cast(u16, (half_t)s) | (u32)__builtin_bit_cast(u16, mid_h) << 16;
-  const float inv = s > 0.f ? 1.0f / s : 0.f;
-  float c[8], off = 0.f;
+  const float inv = s > 0.f ? __builtin_amdgcn_rcpf(s) : 0.f;
+  float c[8], off = 0.f, least = fabsf(mid);
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const float y = (x[i] - mid) * inv, n = rintf(y);
-    off = fmaxf(off, fabsf(y - n));
+    const float d = x[i] - mid, y = d * inv, q = fmaf(fmaf(-y, s, d), inv, y), n = rintf(q);
+    off = fmaxf(off, fabsf(q - n));
+    least = fminf(least, fabsf(x[i]));
     c[i] = __builtin_amdgcn_fmed3f(n, -8.f, 7.f);
   }
-  if (__any(off > 0.49999f)) {
+  if (__any(off > 0.49999f && least < s * 0x1p-9f)) {
     if (s > 0.f) {
+#pragma unroll 1
+      for (int i = 0; i < 8; ++i) {
+        float v = x[0];
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        c[i] = __builtin_amdgcn_fmed3f((float)rint(((double)x[i] - (double)mid) / (double)s), -8.f, 7.f);
+        for (int k = 1; k < 8; ++k) v = k == i ? x[k] : v;
+        v = __builtin_amdgcn_fmed3f((float)rint(((double)v - (double)mid) / (double)s), -8.f, 7.f);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) c[k] = k == i ? v : c[k];
+      }
     }
   }
   auto four = [](float a, float b, float d, float e) {   // c + 8 of four elements in 16 bits: whole numbers, exact
@@ -225,16 +240,16 @@ __device__ __forceinline__ u32 kv4_quantise(const float (&x)[8], u32& param) {
 }
 
 // Rows of k and v into the cache.  A thread takes 8 elements of N consecutive rows, four threads a group.  grid = (blocks of N
-// rows, parts of a row's 2 kv_heads HD / 8 threads).  The cache has a head's rows side by side, so the rows of a block share
+// rows, parts of a row's kv_heads HD / 8 threads, keys and values).  The cache has a head's rows side by side, so the rows of a block share
 // lines of it: written one by one from different XCDs, a line of parameters (8 rows) would leave eight L2s in parts.
 template <class T, int HD, int N>
 __global__ __launch_bounds__(256) void kv4_write_kernel(Kv4Pool p, Kv4Rows r, Kv4View k, Kv4View v) {
   constexpr int UPR = HD / 8;
-  const int i0 = blockIdx.x * N, units = p.kv_heads * UPR, t = blockIdx.y * 256 + threadIdx.x;
-  const int which = t >= units, unit = which ? t - units : t, head = unit / UPR, oct = unit % UPR;
+  const int i0 = blockIdx.x * N, unit = blockIdx.y * blockDim.x + threadIdx.x, which = blockIdx.z;
+  const int head = unit / UPR, oct = unit % UPR;
   int row[N];
   kv4_places<N>(p, r, i0, row);
-  if (t >= 2 * units) return;
+  if (head >= p.kv_heads) return;
   const Kv4View from = which ? v : k;
   u16x8 in[N];
 #pragma unroll
@@ -249,8 +264,8 @@ __global__ __launch_bounds__(256) void kv4_write_kernel(Kv4Pool p, Kv4Rows r, Kv
     for (int i = 0; i < 8; ++i) x[i] = T::load(in[n][i]);
     u32 param;
     const u32 w = kv4_quantise(x, param);
-    *as_global(reinterpret_cast<u32*>(codes + (size_t)row[n] * (HD / 2))) = w;
-    if (oct % 4 == 0) *as_global(reinterpret_cast<u32*>(params + (size_t)row[n] * (HD / 8))) = param;
+    *as_global(reinterpret_cast<u32*>(codes + (size_t)(u32)row[n] * (HD / 2))) = w;
+    if (oct % 4 == 0) *as_global(reinterpret_cast<u32*>(params + (size_t)(u32)row[n] * (HD / 8))) = param;
   }
 }
 
@@ -262,18 +277,18 @@ __device__ __forceinline__ float kv4_value(u32 w, int i, float s, float mid) {
 template <class T, int HD, int N>
 __global__ __launch_bounds__(256) void kv4_read_kernel(Kv4Pool p, Kv4Rows r, Kv4View k, Kv4View v) {
   constexpr int UPR = HD / 8;
-  const int i0 = blockIdx.x * N, units = p.kv_heads * UPR, t = blockIdx.y * 256 + threadIdx.x;
-  const int which = t >= units, unit = which ? t - units : t, head = unit / UPR, oct = unit % UPR;
+  const int i0 = blockIdx.x * N, unit = blockIdx.y * blockDim.x + threadIdx.x, which = blockIdx.z;
+  const int head = unit / UPR, oct = unit % UPR;
   int row[N];
   kv4_places<N>(p, r, i0, row);
-  if (t >= 2 * units) return;
+  if (head >= p.kv_heads) return;
   const Kv4View to = which ? v : k;
   const char *codes = kv4_codes<HD>(p, which, head) + oct * 4, *params = kv4_params<HD>(p, which, head) + oct / 4 * 4;
   u32 w[N], param[N];
 #pragma unroll
   for (int n = 0; n < N; ++n) {
-    w[n] = *as_global(reinterpret_cast<const u32*>(codes + (size_t)max(row[n], 0) * (HD / 2)));
-    param[n] = *as_global(reinterpret_cast<const u32*>(params + (size_t)max(row[n], 0) * (HD / 8)));
+    w[n] = *as_global(reinterpret_cast<const u32*>(codes + (size_t)(u32)max(row[n], 0) * (HD / 2)));
+    param[n] = *as_global(reinterpret_cast<const u32*>(params + (size_t)(u32)max(row[n], 0) * (HD / 8)));
   }
 #pragma unroll
   for (int n = 0; n < N; ++n) {
