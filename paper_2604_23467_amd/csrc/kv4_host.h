@@ -134,7 +134,7 @@ void kv4_launch_attention(hipStream_t s, int32_t dtype, int head_dim, const Kv4P
     if (p16) fresh ? go(kv4_attn_few_kernel<T, HD, true, true>) : go(kv4_attn_few_kernel<T, HD, true, false>);
     else fresh ? go(kv4_attn_few_kernel<T, HD, false, true>) : go(kv4_attn_few_kernel<T, HD, false, false>);
     if (a.splits > 1)
-      hipLaunchKernelGGL((kv4_join_kernel<T, HD>), dim3((unsigned)a.works), dim3(256), 0, s, p, r, o, heads, a.splits, a.row_blocks, part);
+      hipLaunchKernelGGL((kv4_join_kernel<T, HD>), dim3((unsigned)a.works, KV4_FEW_ROWS / 4), dim3(256), 0, s, p, r, o, heads, a.splits, a.row_blocks, part);
   });
 }
 

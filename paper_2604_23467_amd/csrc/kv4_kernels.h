@@ -882,36 +882,42 @@ __global__ __launch_bounds__(256, 3) void kv4_attn_few_kernel(Kv4Pool p, Kv4Rows
   }
 }
 
-// The shares of a row block together: grid = kv_heads * row blocks * sequences
+// The shares of a query row together: a wave a row, a lane a share for the weights, then HD / 64 elements a lane.
+// grid = (kv_heads * row blocks * sequences, 4), the row block's rows dealt to 4 workgroups of four waves
 template <class T, int HD>
 __global__ __launch_bounds__(256) void kv4_join_kernel(Kv4Pool p, Kv4Rows r, Kv4View o, int heads, int splits, int row_blocks,
                                                        const float* part) {
+  typedef float vec __attribute__((ext_vector_type(HD / 64)));
+  constexpr size_t PART = 16 * (HD + 2);
   const Kv4Work w = kv4_work(blockIdx.x, 1, p.kv_heads, row_blocks);
   const Kv4Seq s = kv4_seq(r, w.b);
   const int share_heads = heads / p.kv_heads, rows = min(s.rows, r.max_rows) * share_heads;
-  const int f0 = w.rb * KV4_FEW_ROWS;
-  if (f0 >= rows) return;
+  const int lane = threadIdx.x & 63, row = blockIdx.y * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int f0 = w.rb * KV4_FEW_ROWS, f = f0 + row;
+  if (f >= rows) return;
   const int n_keys = max(s.len - s.rows + min(f0 + KV4_FEW_ROWS - 1, rows - 1) / share_heads + 1, 0);
   const int tiles = (n_keys + KV4_TILE - 1) / KV4_TILE, share = kv4_share(tiles, splits);
   const int n = tiles ? (tiles + share - 1) / share : 1;
-  const float* from = part + (size_t)blockIdx.x * splits * 16 * (HD + 2);
-  for (int i = threadIdx.x; i < min(16, rows - f0) * (HD / 8); i += 256) {
-    const int row = i / (HD / 8), oct = i % (HD / 8), ff = f0 + row, jj = ff / share_heads;
-    float top = -INFINITY;
-    for (int k = 0; k < n; ++k) top = fmaxf(top, from[(size_t)k * 16 * (HD + 2) + 16 * HD + row]);
-    float l = 0.f;
-    f4 a{0.f, 0.f, 0.f, 0.f}, b = a;
-    for (int k = 0; k < n; ++k) {
-      const float* f = from + (size_t)k * 16 * (HD + 2);
-      const float m = f[16 * HD + row], x = m > -INFINITY ? __builtin_amdgcn_exp2f(m - top) : 0.f;
-      l += x * f[16 * HD + 16 + row];
-      a += x * *reinterpret_cast<const f4*>(f + row * HD + oct * 8);
-      b += x * *reinterpret_cast<const f4*>(f + row * HD + oct * 8 + 4);
-    }
-    const float inv = l != 0.f ? 1.0f / l : 0.f;
-    u16x8 v;
+  const float* from = part + (size_t)blockIdx.x * splits * PART;
+  const float m = lane < n ? from[lane * PART + 16 * HD + row] : -INFINITY, l = lane < n ? from[lane * PART + 16 * HD + 16 + row] : 0.f;
+  float top = m;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) { v[e] = T::store(a[e] * inv); v[4 + e] = T::store(b[e] * inv); }
-    kv4_store8(o, s.first + jj, w.head * share_heads + ff - jj * share_heads, oct * 8, v);
+  for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+  const float weight = m > -INFINITY ? __builtin_amdgcn_exp2f(m - top) : 0.f;
+  const float sum = wave_sum(weight * l);
+  const float inv = sum != 0.f ? 1.0f / sum : 0.f;
+  vec a{};
+  const float* at = from + row * HD + lane * (HD / 64);
+  for (int k = 0; k < n; k += 8) {
+    vec v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = *as_global(reinterpret_cast<const vec*>(at + min(k + i, n - 1) * PART));
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (k + i < n) a += v[i] * __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, weight), k + i));
   }
+  const int j = f / share_heads;
+  u16* to = (u16*)o.data + (s.first + j) * o.row_stride + (w.head * share_heads + f - j * share_heads) * o.head_stride + lane * (HD / 64);
+#pragma unroll
+  for (int i = 0; i < HD / 64; ++i) to[i] = T::store(a[i] * inv);
 }
