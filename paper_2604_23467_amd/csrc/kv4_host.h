@@ -102,39 +102,59 @@ void kv4_launch_write(hipStream_t s, int32_t dtype, int head_dim, const Kv4Pool&
   });
 }
 
-// How attention is cut into workgroups: row blocks of 16 query rows, and shares of the keys where that leaves CUs idle
+// How attention is cut into workgroups: blocks of query rows, and shares of the keys where that leaves CUs idle
 struct Kv4Plan {
+  bool many;                   // row blocks of 128, else of 16
   int row_blocks, splits;
   int64_t works;               // (row block, key head, sequence)
   size_t bytes;                // of workspace
 };
+#ifndef KV4_MANY_FROM
+#define KV4_MANY_FROM 64
+#endif
 Kv4Plan kv4_plan(const Kv4Pool& p, const Kv4Rows& r, int max_len, int head_dim, int heads) {
   Kv4Plan a{};
-  a.row_blocks = (int)(((int64_t)r.max_rows * (heads / p.kv_heads) + KV4_FEW_ROWS - 1) / KV4_FEW_ROWS);
+  const int64_t rows = (int64_t)r.max_rows * (heads / p.kv_heads);
+  a.many = rows > KV4_MANY_FROM;
+  const int block = a.many ? KV4_MANY_ROWS : KV4_FEW_ROWS;
+  a.row_blocks = (int)((rows + block - 1) / block);
   a.works = (int64_t)a.row_blocks * p.kv_heads * r.n_seqs;
   const int64_t most = (int64_t)r.table_stride * p.page_tokens;
   const int64_t len = max_len > 0 ? std::min<int64_t>(max_len, most) : most;
   const int64_t rounds = (len + KV4_TILE * KV4_WAVES - 1) / (KV4_TILE * KV4_WAVES);      // of the four waves over the keys
   const int64_t want = (2 * num_cus() + a.works - 1) / std::max<int64_t>(a.works, 1);
-  a.splits = (int)std::max<int64_t>(1, std::min<int64_t>({want, rounds / 4, 64}));
-  if (a.splits > 1) a.bytes = align_up((size_t)a.works * a.splits * 16 * (head_dim + 2) * sizeof(float));
+  a.splits = (int)std::max<int64_t>(1, std::min<int64_t>({want, rounds / 4, 64}));       // (64: a wave's lanes, see the join)
+  if (a.splits > 1) a.bytes = align_up((size_t)a.works * a.splits * block * (head_dim + 2) * sizeof(float));
   return a;
 }
 
 void kv4_launch_attention(hipStream_t s, int32_t dtype, int head_dim, const Kv4Pool& p, const Kv4Rows& r, int heads, float scale,
                           const Kv4View& q, const Kv4View* k, const Kv4View* v, const Kv4View& o, const Kv4Plan& a, float* part) {
+  const bool fresh = k && r.max_rows == 1 && !a.many;
+  if (k && !fresh) kv4_launch_write(s, dtype, head_dim, p, r, *k, *v);
   kv4_dispatch(dtype, head_dim, [&](auto t, auto hd) {
     using T = decltype(t);
     constexpr int HD = decltype(hd)::value;
     const dim3 grid((unsigned)(a.works * a.splits));
-    const bool p16 = p.page_tokens % 16 == 0, fresh = k && r.max_rows == 1;
+    const bool p16 = p.page_tokens % 16 == 0;
+    if (a.many) {
+      auto go = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, p, r, q, o, heads, scale, a.splits, a.row_blocks, part);
+      };
+      p16 ? go(kv4_attn_many_kernel<T, HD, true>) : go(kv4_attn_many_kernel<T, HD, false>);
+      if (a.splits > 1)
+        hipLaunchKernelGGL((kv4_join_kernel<T, HD, KV4_MANY_ROWS>), dim3((unsigned)a.works, KV4_MANY_ROWS / 4), dim3(256), 0, s, p, r, o,
+                           heads, a.splits, a.row_blocks, part);
+      return;
+    }
     auto go = [&](auto kernel) {
       hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, p, r, q, o, fresh ? *k : q, fresh ? *v : q, heads, scale, a.splits, a.row_blocks, part);
     };
     if (p16) fresh ? go(kv4_attn_few_kernel<T, HD, true, true>) : go(kv4_attn_few_kernel<T, HD, true, false>);
     else fresh ? go(kv4_attn_few_kernel<T, HD, false, true>) : go(kv4_attn_few_kernel<T, HD, false, false>);
     if (a.splits > 1)
-      hipLaunchKernelGGL((kv4_join_kernel<T, HD>), dim3((unsigned)a.works, KV4_FEW_ROWS / 4), dim3(256), 0, s, p, r, o, heads, a.splits, a.row_blocks, part);
+      hipLaunchKernelGGL((kv4_join_kernel<T, HD, KV4_FEW_ROWS>), dim3((unsigned)a.works, KV4_FEW_ROWS / 4), dim3(256), 0, s, p, r, o, heads,
+                         a.splits, a.row_blocks, part);
   });
 }
 
@@ -221,7 +241,6 @@ int ll_kv4_attention(const ll_kv4_cache* cache, const ll_kv4_rows* rows, int32_t
   if (a.bytes && reinterpret_cast<uintptr_t>(workspace) % kAlign)
     return fail(LL_E_WORKSPACE, "%s: workspace must be %zu-byte aligned", who, kAlign);
   const hipStream_t s = static_cast<hipStream_t>(hip_stream);
-  if (k && r.max_rows > 1) kv4_launch_write(s, dtype, cache->head_dim, p, r, kk, vv);
   if (scale == 0.f) scale = 1.0f / sqrtf((float)cache->head_dim);
   kv4_launch_attention(s, dtype, cache->head_dim, p, r, n_heads, scale, qq, k ? &kk : nullptr, k ? &vv : nullptr, oo, a,
                        static_cast<float*>(workspace));

@@ -882,24 +882,326 @@ __global__ __launch_bounds__(256, 3) void kv4_attn_few_kernel(Kv4Pool p, Kv4Rows
   }
 }
 
+// ---- many query rows ----
+//
+// 128 query rows of one key head, 32 a wave.  Here the products count, and the 32x32x16 form has the higher rate; codes are
+// turned into operands once for all four waves: every wave does so for 32 of a tile's 128 keys and leaves the fragments in
+// LDS, 16 bytes a lane and side by side, as the waves read them.  With lane = 32 h + c, a product's rows and columns c and its
+// contraction 8 h + i, the operands follow the same ideas as above:
+//  * K: half h of key c's row, 8 elements a product, and a product of the middles (two groups a half with head_dim 128);
+//  * S^T leaves the lane with keys 8 a + 4 h + b (a, b < 4) of query c; product n of V^T P^T contracts over a = 2 n and 2 n + 1;
+//  * V: row c of block e is element (HD / 32) c + e, and the lane's outputs are HD / 8 elements in a row for every a, of group a
+//    (head_dim 64: a / 2).  Rows of the further block: 4 x the group's middle, 4 x + 1 ones, 4 x + 2 the group's NaN marks.
+// Weights enter as one binary16 number here: their rounding is as large as that of a binary16 output.
+#define KV4_MANY_ROWS 128
+
+__device__ __forceinline__ f16v kv4_mfma(h8 a, h8 b, f16v c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ float kv4_max_over_halves(float v) {
+  const u32 b = __builtin_bit_cast(u32, v);
+  const auto r = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+  return fmaxf(__builtin_bit_cast(float, (u32)r[0]), __builtin_bit_cast(float, (u32)r[1]));
+}
+// all of a workgroup's waves, without waiting for loads in flight
+__device__ __forceinline__ void kv4_barrier() {
+  wait_lgkm_at_most<0>();
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+template <int HD>
+struct Kv4Operands {
+  static constexpr int KS = HD / 16, NE = HD / 32;            // products of a score; row blocks of elements
+  static constexpr int FRAGS = KS + 1 + 2 * (NE + 1);         // fragments of 32 keys
+};
+
+// 32 keys as they lie in the pool: half h of key c's row, the lane's (HD / 32) elements of 16 values
+template <int HD>
+struct Kv4Raw {
+  u32x4 k[HD / 64];
+  u32x2 kp;
+  u32 v[16], vp[16];
+};
+
+template <class T, int HD, bool P16>
+__global__ __launch_bounds__(256, 2) void kv4_attn_many_kernel(Kv4Pool p, Kv4Rows r, Kv4View q, Kv4View o, int heads, float scale,
+                                                               int splits, int row_blocks, float* part) {
+  using Op = Kv4Operands<HD>;
+  constexpr int KS = Op::KS, NE = Op::NE;
+  __shared__ __attribute__((aligned(16))) h8 s_frag[KV4_WAVES][Op::FRAGS][64];
+  __shared__ __attribute__((aligned(16))) u32 s_rows[P16 ? 1 : KV4_WAVES][KV4_TILE];
+  __shared__ u32 s_has[KV4_WAVES];
+  Kv4Work w = kv4_work(blockIdx.x, splits, p.kv_heads, row_blocks);
+  w.rb = row_blocks - 1 - w.rb;                                            // the longest first
+  const int tid = threadIdx.x, lane = tid & 63, c = lane & 31, h = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const Kv4Seq s = kv4_seq(r, w.b);
+  const int share_heads = heads / p.kv_heads, rows = min(s.rows, r.max_rows) * share_heads;
+  const int f0 = w.rb * KV4_MANY_ROWS;
+  if (f0 >= rows) return;
+  const int n_keys = max(s.len - s.rows + min(f0 + KV4_MANY_ROWS - 1, rows - 1) / share_heads + 1, 0);
+  const int tiles = (n_keys + KV4_TILE - 1) / KV4_TILE, share = kv4_share(tiles, splits);
+  const int t0 = w.split * share, t1 = min(t0 + share, tiles);
+  if (w.split > 0 && t0 >= tiles) return;
+  const int* table = r.table + (size_t)w.b * r.table_stride;
+
+  const int fw = f0 + wave * 32, f = fw + c, j = f / share_heads, qhead = w.head * share_heads + f - j * share_heads;
+  const bool there = f < rows;
+  const int limit = there ? s.len - s.rows + j : -1;
+  const int first_limit = s.len - s.rows + fw / share_heads;               // of the wave's queries
+  const int last_limit = fw < rows ? s.len - s.rows + min(fw + 31, rows - 1) / share_heads : -1;
+
+  // Pool rows of the wave's part (32 keys) of a tile
+  const int ahead = P16 ? 0 : c;
+  auto page = [&](int u) { return (int)(__umulhi((u32)u << 1, p.magic) >> p.shift); };
+  auto look = [&](int t) {
+    const int last = r.table_stride - 1, u = t * KV4_TILE + ahead;
+    if constexpr (P16) return u32x2{(u32)kv4_scalar(table + min(page(u), last)), (u32)kv4_scalar(table + min(page(u + 16), last))};
+    else return u32x2{(u32)*as_global(table + min(page(u), last)), 0};
+  };
+  auto row = [&](int u, u32 at) {
+    const int pg = page(u);
+    return u < n_keys && pg < r.table_stride && at <= (u32)(p.pool_rows - p.page_tokens) ? (int)(at + (u - pg * p.page_tokens)) : -1;
+  };
+  auto place = [&](int t, u32x2 at, u32& has) {
+    const int u = t * KV4_TILE + ahead;
+    if constexpr (P16) {
+      const int a = row(u, at[0]), b = row(u + 16, at[1]);
+      const u32 one = a >= 0 ? 0xffffu >> max(u + 16 - n_keys, 0) : 0u, two = b >= 0 ? 0xffffu >> max(u + 32 - n_keys, 0) : 0u;
+      has = one | two << 16;
+      return Kv4Halves{u32x2{(u32)max(a, 0), (u32)max(b, 0)}};
+    } else {
+      const int a = row(u, at[0]);
+      has = (u32)__ballot(a >= 0);
+      s_rows[wave][ahead] = max(a, 0);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      return Kv4Listed{s_rows[wave]};
+    }
+  };
+  const char *kc = kv4_codes<HD>(p, 0, w.head), *kp = kv4_params<HD>(p, 0, w.head);
+  const char *vc = kv4_codes<HD>(p, 1, w.head), *vp = kv4_params<HD>(p, 1, w.head);
+  Kv4Raw<HD> raw;
+  u32 has = 0;
+  auto fetch = [&](const auto& where) {
+    const char* a = where.split(kc, HD / 2, c) + h * (HD / 4);
+#pragma unroll
+    for (int n = 0; n < HD / 64; ++n) raw.k[n] = *as_global(reinterpret_cast<const u32x4*>(a + 16 * n));
+    const char* b = where.split(kp, HD / 8, c) + h * (HD / 16);
+    if (HD == 128) raw.kp = *as_global(reinterpret_cast<const u32x2*>(b));
+    else raw.kp = u32x2{*as_global(reinterpret_cast<const u32*>(b)), 0};
+#pragma unroll
+    for (int n = 0; n < 16; ++n) {                     // key 16 (n / 8) + 8 (n / 4 % 2) + 4 h + n % 4
+      const u32 i = 8 * (n >> 2 & 1) + 4 * h + (n & 3);
+      const char* x = where.at(vc, HD / 2, n >> 3, i) + c * (HD / 64);
+      raw.v[n] = HD == 128 ? (u32)*as_global(reinterpret_cast<const u16*>(x)) : (u32)*as_global(reinterpret_cast<const unsigned char*>(x));
+      raw.vp[n] = *as_global(reinterpret_cast<const u32*>(where.at(vp, HD / 8, n >> 3, i) + (c * (HD / 32) / KV4_GROUP) * 4));
+    }
+  };
+  const Kv4Bits bits;
+  // the wave's 32 keys as fragments: K's KS, their middles, then for either half of the keys V's NE and theirs
+  auto produce = [&]() {
+    h8(*out)[64] = s_frag[wave];
+#pragma unroll
+    for (int n = 0; n < KS; ++n) {
+      const u32 g = HD == 128 ? raw.kp[n >> 2] : raw.kp[0];
+      const h2 step = kv4_h2(kv4_lo16(g, g));
+      h2 d[4];
+      bits.unpack(raw.k[n >> 2][n & 3], d);
+      out[n][lane] = __builtin_bit_cast(h8, u32x4{kv4_u32(d[0] * step), kv4_u32(d[1] * step), kv4_u32(d[2] * step), kv4_u32(d[3] * step)});
+    }
+    const half_t m0 = kv4_h2(raw.kp[0])[1], m1 = HD == 128 ? kv4_h2(raw.kp[1])[1] : (half_t)0;
+    out[KS][lane] = h8{m0, m0, m0, m1, m1, m1, 0, 0};
+    u32 marks = 0;
+    h2 all = kv4_h2(raw.vp[0]);
+#pragma unroll
+    for (int n = 1; n < 16; ++n) all += kv4_h2(raw.vp[n]);
+    if (~has || __any(!(all[1] == all[1]))) {
+#pragma unroll
+      for (int n = 0; n < 16; ++n) {
+        const half_t mid = kv4_h2(raw.vp[n])[1];
+        const int key = 16 * (n >> 3) + 8 * (n >> 2 & 1) + 4 * h + (n & 3);
+        const bool gone = !(has >> key & 1), nan = !(mid == mid);
+        if (nan && !gone) marks |= 1u << n;
+        if (gone || nan) raw.vp[n] = 0;
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      u32x4 w4[4], mids;
+#pragma unroll
+      for (int a = 0; a < 4; ++a) {
+        const int n = 8 * t + 2 * a;
+        const h2 step = kv4_h2(kv4_lo16(raw.vp[n], raw.vp[n + 1]));
+        h2 d[4];
+        bits.unpack(raw.v[n] | raw.v[n + 1] << 16, d);
+#pragma unroll
+        for (int i = 0; i < NE; ++i) w4[i][a] = kv4_u32(d[i] * step);
+        const u32 mark = (marks >> n & 1 ? 0x3c00u : 0u) | (marks >> (n + 1) & 1 ? 0x3c000000u : 0u);
+        mids[a] = (c & 3) == 0 ? kv4_hi16(raw.vp[n], raw.vp[n + 1]) : (c & 3) == 1 ? 0x3c003c00u : (c & 3) == 2 ? mark : 0u;
+      }
+#pragma unroll
+      for (int i = 0; i < NE; ++i) out[KS + 1 + t * (NE + 1) + i][lane] = __builtin_bit_cast(h8, w4[i]);
+      out[KS + 1 + t * (NE + 1) + NE][lane] = __builtin_bit_cast(h8, mids);
+    }
+    if (lane == 0) s_has[wave] = has;
+  };
+
+  u32x2 at{0, 0};
+  if (t0 < t1) {
+    const u32x2 at0 = look(t0 + wave);
+    at = look(t0 + KV4_WAVES + wave);
+    fetch(place(t0 + wave, at0, has));
+  }
+  // queries, in K's order and scaled as above
+  h8 qf[KS], sums;
+  float qscale;
+  {
+    float x[KS][8], top = 0.f;
+#pragma unroll
+    for (int n = 0; n < KS; ++n) {
+      u16x8 in{};
+      if (there) in = kv4_load8(q, s.first + j, qhead, h * (HD / 2) + n * 8);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        x[n][i] = T::load(in[i]);
+        top = fmaxf(top, fabsf(x[n][i]));
+      }
+    }
+    top = kv4_max_over_halves(top);
+    int e = 0;
+    if (top > 0.f && top < INFINITY) e = ilogbf(top);
+    float sum[2] = {0.f, 0.f};
+#pragma unroll
+    for (int n = 0; n < KS; ++n)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const half_t a = (half_t)ldexpf(x[n][i], -e), b = (half_t)ldexpf(x[n][i + 4], -e);
+        qf[n][2 * i] = a;
+        qf[n][2 * i + 1] = b;
+        sum[n >> 2] += (float)a + (float)b;
+      }
+    half_t y[2][3];
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      y[g][0] = (half_t)sum[g];
+      y[g][1] = (half_t)(sum[g] - (float)y[g][0]);
+      y[g][2] = (half_t)(sum[g] - (float)y[g][0] - (float)y[g][1]);
+    }
+    sums = h8{y[0][0], y[0][1], y[0][2], y[1][0], y[1][1], y[1][2], 0, 0};
+    qscale = fmaxf(ldexpf(scale * 1.44269504088896340736f, e), 0x1p-126f);
+  }
+
+  f16v acc[NE + 1];
+#pragma unroll
+  for (int e = 0; e <= NE; ++e)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) acc[e][i] = 0.f;
+  float m = -INFINITY;
+  for (int t = t0; t < t1; t += KV4_WAVES) {
+    produce();
+    if (t + KV4_WAVES < t1) {
+      const u32x2 now = at;
+      at = look(t + 2 * KV4_WAVES + wave);
+      fetch(place(t + KV4_WAVES + wave, now, has));
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    kv4_barrier();
+    for (int n = 0; n < KV4_WAVES; ++n) {
+      const int u0 = (t + n) * KV4_TILE;
+      if (u0 > last_limit || u0 >= n_keys) break;
+      const u32 there_mask = __builtin_amdgcn_readfirstlane(s_has[n]);
+      const h8(*in)[64] = s_frag[n];
+      f16v sc;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sc[i] = 0.f;
+      sc = kv4_mfma(in[KS][lane], sums, sc);
+#pragma unroll
+      for (int i = 0; i < KS; ++i) sc = kv4_mfma(in[i][lane], qf[i], sc);
+      float x[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x[i] = sc[i] * qscale;
+      if (u0 + KV4_TILE - 1 > first_limit || ~there_mask) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int key = 8 * (i >> 2) + 4 * h + (i & 3);
+          if (!(there_mask >> key & 1) || u0 + key > limit) x[i] = -INFINITY;
+        }
+      }
+      float top = x[0];
+#pragma unroll
+      for (int i = 1; i < 16; ++i) top = fmaxf(top, x[i]);
+      top = fmaxf(kv4_max_over_halves(top), m);
+      if (__any(top > m)) {
+        const float corr = top > m ? __builtin_amdgcn_exp2f(m - top) : 1.0f;
+        m = top;
+#pragma unroll
+        for (int e = 0; e <= NE; ++e) acc[e] *= corr;
+      }
+      const float base = KV4_SHIFT - (m > -INFINITY ? m : 0.f);
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        h8 pr;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) pr[i] = (half_t)__builtin_amdgcn_exp2f(x[8 * k + i] + base);
+#pragma unroll
+        for (int e = 0; e <= NE; ++e) acc[e] = kv4_mfma(in[KS + 1 + k * (NE + 1) + e][lane], pr, acc[e]);
+      }
+    }
+    kv4_barrier();
+  }
+
+  // outputs: element (HD / 32) (8 a + 4 h + b) + e is register 4 a + b of block e
+  if (!there) return;
+  const float l = acc[NE][1], inv = splits > 1 ? 1.0f : l != 0.f ? 1.0f / l : 0.f;
+  float* to = part + (size_t)blockIdx.x * KV4_MANY_ROWS * (HD + 2);
+  const int at_row = wave * 32 + c;
+#pragma unroll
+  for (int a = 0; a < 4; ++a) {
+    const float mid = acc[NE][4 * a + 2] != 0.f ? NAN : acc[NE][4 * a];
+    float y[HD / 8];
+#pragma unroll
+    for (int b = 0; b < 4; ++b)
+#pragma unroll
+      for (int e = 0; e < NE; ++e) y[b * NE + e] = (acc[e][4 * a + b] + mid) * inv;
+    const int e0 = (HD / 32) * (8 * a + 4 * h);
+#pragma unroll
+    for (int n = 0; n < HD / 64; ++n) {
+      if (splits == 1) {
+        u16x8 v;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = T::store(y[8 * n + i]);
+        kv4_store8(o, s.first + j, qhead, e0 + 8 * n, v);
+      } else {
+        *reinterpret_cast<f4*>(to + at_row * HD + e0 + 8 * n) = f4{y[8 * n], y[8 * n + 1], y[8 * n + 2], y[8 * n + 3]};
+        *reinterpret_cast<f4*>(to + at_row * HD + e0 + 8 * n + 4) = f4{y[8 * n + 4], y[8 * n + 5], y[8 * n + 6], y[8 * n + 7]};
+      }
+    }
+  }
+  if (splits > 1 && h == 0) {
+    to[KV4_MANY_ROWS * HD + at_row] = m;
+    to[KV4_MANY_ROWS * HD + KV4_MANY_ROWS + at_row] = l;
+  }
+}
+
 // The shares of a query row together: a wave a row, a lane a share for the weights, then HD / 64 elements a lane.
-// grid = (kv_heads * row blocks * sequences, 4), the row block's rows dealt to 4 workgroups of four waves
-template <class T, int HD>
+// grid = (kv_heads * row blocks * sequences, ROWS / 4)
+template <class T, int HD, int ROWS>
 __global__ __launch_bounds__(256) void kv4_join_kernel(Kv4Pool p, Kv4Rows r, Kv4View o, int heads, int splits, int row_blocks,
                                                        const float* part) {
   typedef float vec __attribute__((ext_vector_type(HD / 64)));
-  constexpr size_t PART = 16 * (HD + 2);
-  const Kv4Work w = kv4_work(blockIdx.x, 1, p.kv_heads, row_blocks);
+  constexpr size_t PART = ROWS * (HD + 2);
+  Kv4Work w = kv4_work(blockIdx.x, 1, p.kv_heads, row_blocks);
+  if (ROWS > KV4_FEW_ROWS) w.rb = row_blocks - 1 - w.rb;
   const Kv4Seq s = kv4_seq(r, w.b);
   const int share_heads = heads / p.kv_heads, rows = min(s.rows, r.max_rows) * share_heads;
   const int lane = threadIdx.x & 63, row = blockIdx.y * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int f0 = w.rb * KV4_FEW_ROWS, f = f0 + row;
+  const int f0 = w.rb * ROWS, f = f0 + row;
   if (f >= rows) return;
-  const int n_keys = max(s.len - s.rows + min(f0 + KV4_FEW_ROWS - 1, rows - 1) / share_heads + 1, 0);
+  const int n_keys = max(s.len - s.rows + min(f0 + ROWS - 1, rows - 1) / share_heads + 1, 0);
   const int tiles = (n_keys + KV4_TILE - 1) / KV4_TILE, share = kv4_share(tiles, splits);
   const int n = tiles ? (tiles + share - 1) / share : 1;
   const float* from = part + (size_t)blockIdx.x * splits * PART;
-  const float m = lane < n ? from[lane * PART + 16 * HD + row] : -INFINITY, l = lane < n ? from[lane * PART + 16 * HD + 16 + row] : 0.f;
+  const float m = lane < n ? from[lane * PART + ROWS * HD + row] : -INFINITY, l = lane < n ? from[lane * PART + ROWS * HD + ROWS + row] : 0.f;
   float top = m;
 #pragma unroll
   for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
