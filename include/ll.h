@@ -255,6 +255,13 @@ size_t ll_batch_pool_bytes(int32_t page_tokens, int32_t n_pages);
  * up to 16 slots, 32 beyond).  LL_E_BAD_CONFIG unless
  * d_model % 16 == 0, d_model <= 4096, ffn_hidden % 8 == 0, vocab % 16 == 0, head_dim 64 or 128. */
 int ll_batch_open(int32_t max_batch, int32_t page_tokens, int32_t n_pages, void *pool, size_t pool_bytes);
+/* The two calls with a choice of what an element of the cache is held in: kv_bits = 16 (binary16, as above) or 4 (five bits with
+ * what belongs to them, see the 4-bit cache below: less than a third of the bytes to keep and to read, for values that are
+ * off by up to half a step).  With 4 bits a prompt's rows are quantised as they move into the pages, a step's as they are
+ * written; attention uses them as they are held, the newest included.  LL_E_BAD_ARG for other kv_bits, and for
+ * page_tokens * n_pages > 2^26 with 4. */
+size_t ll_batch_pool_bytes_kv(int32_t page_tokens, int32_t n_pages, int32_t kv_bits);
+int ll_batch_open_kv(int32_t max_batch, int32_t page_tokens, int32_t n_pages, int32_t kv_bits, void *pool, size_t pool_bytes);
 /* Adds a sequence: prefills tokens[0..n) (host pointer), moves its cache rows into freshly taken
  * pages, stores the first generated token in *first_token and returns the slot (>= 0) the sequence
  * occupies.  LL_E_CAPACITY when no slot or not enough pages are free, or n + 1 > max_seq; those and
@@ -276,6 +283,9 @@ int ll_batch_close(void);
  * k steps write are taken first, LL_E_CAPACITY and nothing run if the pool cannot supply them). */
 int ll_batch_dbg_get_logits(int32_t slot, float *host_out);
 int ll_batch_dbg_force_next_token(int32_t slot, int32_t tok);
+/* Cached keys (which = 0) or values (which = 1) of one layer of `slot`, positions [0, n_pos) with n_pos at most the slot's
+ * cached positions, converted to float, laid out [n_pos][d_model] on the host. */
+int ll_batch_dbg_get_kv(int32_t slot, int32_t layer, int32_t which, int32_t n_pos, float *host_out);
 int ll_batch_dbg_time_steps(int32_t k, float *ms_out);
 
 /* ---- a key/value cache held in 4 bits ----
@@ -289,7 +299,8 @@ int ll_batch_dbg_time_steps(int32_t k, float *ms_out);
  * The three calls below work on one layer's pool, with or without an initialised instance, on the stream that they are given
  * (a hipStream_t; NULL: the default stream) of the current device, which the memory has to belong to.  They return when their
  * kernels are queued, hold no state between calls, allocate nothing, and can be captured into a graph.  Every pointer is a
- * DEVICE pointer and stays the caller's.  ll_batch_open_kv runs batched decoding on such pools.
+ * DEVICE pointer and stays the caller's.  ll_batch_open_kv runs batched
+ * decoding on such pools.
  * Errors as above: LL_E_BAD_ARG, LL_E_BAD_CONFIG (a shape that is not supported), LL_E_WORKSPACE (pool or workspace too small
  * or misaligned), LL_E_HIP; but for LL_E_HIP nothing was queued. */
 enum { LL_F16 = 0, LL_BF16 = 1 }; /* type of the rows at the calls' borders: binary16, bfloat16 */

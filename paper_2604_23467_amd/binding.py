@@ -31,6 +31,7 @@ EXPORTS = ("ll_workspace_bytes", "ll_init", "ll_prefill", "ll_prefill_static", "
            "ll_set_sampling", "ll_shutdown", "ll_max_prompt", "ll_position", "ll_decode_mode", "ll_last_error", "ll_dbg_get_logits",
            "ll_batch_pool_bytes", "ll_batch_open", "ll_batch_add", "ll_batch_step", "ll_batch_remove", "ll_batch_close",
            "ll_kv4_pool_bytes", "ll_kv4_write", "ll_kv4_read", "ll_kv4_attention_workspace_bytes", "ll_kv4_attention",
+           "ll_batch_pool_bytes_kv", "ll_batch_open_kv", "ll_batch_dbg_get_kv",
            "ll_batch_dbg_get_logits", "ll_batch_dbg_force_next_token", "ll_batch_dbg_time_steps",
            "ll_dbg_get_hidden", "ll_dbg_set_spin_limit", "ll_dbg_give_up_at", "ll_dbg_small_plan", "ll_dbg_graph_stats", "ll_dbg_gemm_plan", "ll_dbg_gemm_slice_count", "ll_dbg_tile_plan", "ll_dbg_batch_order", "ll_dbg_force_next_token", "ll_dbg_get_kv", "ll_dbg_profile_decode",
            "ll_dbg_time_decode", "ll_dbg_time_kernel_class", "ll_dbg_stream_copy", "ll_dbg_stream_read", "ll_dbg_poison_scratch", "ll_dbg_trace_decode")
@@ -111,6 +112,12 @@ def load():
     L.ll_batch_pool_bytes.argtypes = [C.c_int32, C.c_int32]
     L.ll_batch_open.restype = C.c_int
     L.ll_batch_open.argtypes = [C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_size_t]
+    L.ll_batch_pool_bytes_kv.restype = C.c_size_t
+    L.ll_batch_pool_bytes_kv.argtypes = [C.c_int32] * 3
+    L.ll_batch_open_kv.restype = C.c_int
+    L.ll_batch_open_kv.argtypes = [C.c_int32] * 4 + [C.c_void_p, C.c_size_t]
+    L.ll_batch_dbg_get_kv.restype = C.c_int
+    L.ll_batch_dbg_get_kv.argtypes = [C.c_int32] * 4 + [C.POINTER(C.c_float)]
     L.ll_batch_add.restype = C.c_int32
     L.ll_batch_add.argtypes = [C.POINTER(C.c_int32), C.c_int32, C.POINTER(C.c_int32)]
     L.ll_batch_step.restype = C.c_int
@@ -488,14 +495,15 @@ class Session:
         return out
 
     # ---- batched decoding over a paged KV cache ----
-    def ll_batch_open(self, max_batch, page_tokens, n_pages):
-        nbytes = int(self.lib.ll_batch_pool_bytes(page_tokens, n_pages))
+    def ll_batch_open(self, max_batch, page_tokens, n_pages, kv_bits=16):
+        """kv_bits: what an element of the paged cache is held in, 16 or 4 (see ll_batch_open_kv)."""
+        nbytes = int(self.lib.ll_batch_pool_bytes_kv(page_tokens, n_pages, kv_bits))
         if nbytes == 0:
             raise LLError(LL_E_BAD_ARG, "ll_batch_pool_bytes rejected the arguments")
         self.pool = self.torch.empty(nbytes + 256, dtype=self.torch.uint8, device=self.device)
         ptr = (self.pool.data_ptr() + 255) // 256 * 256
         self.max_batch = max_batch
-        return _check(self.lib.ll_batch_open(max_batch, page_tokens, n_pages, C.c_void_p(ptr), C.c_size_t(nbytes)))
+        return _check(self.lib.ll_batch_open_kv(max_batch, page_tokens, n_pages, kv_bits, C.c_void_p(ptr), C.c_size_t(nbytes)))
 
     def ll_batch_add(self, tokens):
         arr = (C.c_int32 * len(tokens))(*[int(t) for t in tokens])
@@ -519,6 +527,11 @@ class Session:
     def ll_batch_dbg_get_logits(self, slot):
         out = np.empty(self.cfg["vocab"], dtype=np.float32)
         _check(self.lib.ll_batch_dbg_get_logits(slot, out.ctypes.data_as(C.POINTER(C.c_float))))
+        return out
+
+    def ll_batch_dbg_get_kv(self, slot, layer, which, n_pos):
+        out = np.empty((n_pos, self.cfg["d_model"]), dtype=np.float32)
+        _check(self.lib.ll_batch_dbg_get_kv(slot, layer, which, n_pos, out.ctypes.data_as(C.POINTER(C.c_float))))
         return out
 
     def ll_batch_dbg_force_next_token(self, slot, tok):

@@ -1,4 +1,4 @@
-// Host side of the 4-bit key/value cache's calls: checks, launch shapes, launches.
+// Host side of the 4-bit key/value cache: checks, launch shapes, launches.  Part of ll_runtime.hip, in front of what uses it.
 #pragma once
 #include "kv4_kernels.h"
 
@@ -65,6 +65,7 @@ int kv4_check_view(const char* who, const char* name, const ll_kv4_view* v, cons
     if (!apart_heads || !apart_rows || !nested)
       return fail(LL_E_BAD_ARG, "%s: strides %lld, %lld make elements of %s overlap", who, (long long)row, (long long)head, name);
   }
+  *out = Kv4View{};
   out->data = v->data;
   out->row_stride = v->row_stride;
   out->head_stride = v->head_stride;
@@ -87,17 +88,26 @@ void kv4_dispatch(int32_t dtype, int head_dim, F&& go) {
 // Blocks of 8 rows where that leaves every CU with work of several workgroups; single rows, whose chain is shorter, else
 constexpr int kKv4RowBlock = 8;
 template <class F>
-void kv4_row_blocks(const Kv4Pool& p, const Kv4Rows& r, int head_dim, F&& go) {
+void kv4_row_blocks(const Kv4Pool& p, const Kv4Rows& r, int head_dim, int layers, F&& go) {
   const int units = p.kv_heads * (head_dim / 8), threads = std::min(256, (units + 63) / 64 * 64), parts = (units + threads - 1) / threads;
-  if ((int64_t)r.n_rows * parts * 2 >= (int64_t)2 * kKv4RowBlock * num_cus())
-    go(Kv4Dim<kKv4RowBlock>{}, dim3((r.n_rows + kKv4RowBlock - 1) / kKv4RowBlock, parts, 2), dim3(threads));
-  else go(Kv4Dim<1>{}, dim3(r.n_rows, parts, 2), dim3(threads));
+  if ((int64_t)r.n_rows * parts * 2 * layers >= (int64_t)2 * kKv4RowBlock * num_cus())
+    go(Kv4Dim<kKv4RowBlock>{}, dim3((r.n_rows + kKv4RowBlock - 1) / kKv4RowBlock, parts, 2 * layers), dim3(threads));
+  else go(Kv4Dim<1>{}, dim3(r.n_rows, parts, 2 * layers), dim3(threads));
 }
 
-void kv4_launch_write(hipStream_t s, int32_t dtype, int head_dim, const Kv4Pool& p, const Kv4Rows& r, const Kv4View& k, const Kv4View& v) {
+void kv4_launch_write(hipStream_t s, int32_t dtype, int head_dim, const Kv4Pool& p, const Kv4Rows& r, const Kv4View& k, const Kv4View& v,
+                      int layers = 1) {
   kv4_dispatch(dtype, head_dim, [&](auto t, auto hd) {
-    kv4_row_blocks(p, r, head_dim, [&](auto n, dim3 grid, dim3 threads) {
+    kv4_row_blocks(p, r, head_dim, layers, [&](auto n, dim3 grid, dim3 threads) {
       hipLaunchKernelGGL((kv4_write_kernel<decltype(t), decltype(hd)::value, decltype(n)::value>), grid, threads, 0, s, p, r, k, v);
+    });
+  });
+}
+
+void kv4_launch_read(hipStream_t s, int32_t dtype, int head_dim, const Kv4Pool& p, const Kv4Rows& r, const Kv4View& k, const Kv4View& v) {
+  kv4_dispatch(dtype, head_dim, [&](auto t, auto hd) {
+    kv4_row_blocks(p, r, head_dim, 1, [&](auto n, dim3 grid, dim3 threads) {
+      hipLaunchKernelGGL((kv4_read_kernel<decltype(t), decltype(hd)::value, decltype(n)::value>), grid, threads, 0, s, p, r, k, v);
     });
   });
 }
@@ -109,21 +119,22 @@ struct Kv4Plan {
   int64_t works;               // (row block, key head, sequence)
   size_t bytes;                // of workspace
 };
-#ifndef KV4_MANY_FROM
-#define KV4_MANY_FROM 64
-#endif
 Kv4Plan kv4_plan(const Kv4Pool& p, const Kv4Rows& r, int max_len, int head_dim, int heads) {
   Kv4Plan a{};
   const int64_t rows = (int64_t)r.max_rows * (heads / p.kv_heads);
-  a.many = rows > KV4_MANY_FROM;
-  const int block = a.many ? KV4_MANY_ROWS : KV4_FEW_ROWS;
-  a.row_blocks = (int)((rows + block - 1) / block);
-  a.works = (int64_t)a.row_blocks * p.kv_heads * r.n_seqs;
   const int64_t most = (int64_t)r.table_stride * p.page_tokens;
   const int64_t len = max_len > 0 ? std::min<int64_t>(max_len, most) : most;
   const int64_t rounds = (len + KV4_TILE * KV4_WAVES - 1) / (KV4_TILE * KV4_WAVES);      // of the four waves over the keys
+  const int64_t shares = std::max<int64_t>(1, std::min<int64_t>(rounds / 4, 64));        // at most (64: a wave's lanes, see the join)
+  // Blocks of 128 rows where they, times the shares, leave no CU idle.  One sequence of 500 rows and 32 heads, 128 such
+  // workgroups: 28.6 us, in blocks of 16 rows 21.2; six of up to 700 behind up to 2000, 1056 workgroups: 120, 160.
+  const int64_t many = (rows + KV4_MANY_ROWS - 1) / KV4_MANY_ROWS * p.kv_heads * r.n_seqs;
+  a.many = rows > KV4_MANY_ROWS / 2 && many * shares >= num_cus();
+  const int block = a.many ? KV4_MANY_ROWS : KV4_FEW_ROWS;
+  a.row_blocks = (int)((rows + block - 1) / block);
+  a.works = (int64_t)a.row_blocks * p.kv_heads * r.n_seqs;
   const int64_t want = (2 * num_cus() + a.works - 1) / std::max<int64_t>(a.works, 1);
-  a.splits = (int)std::max<int64_t>(1, std::min<int64_t>({want, rounds / 4, 64}));       // (64: a wave's lanes, see the join)
+  a.splits = (int)std::min<int64_t>(want, shares);
   if (a.splits > 1) a.bytes = align_up((size_t)a.works * a.splits * block * (head_dim + 2) * sizeof(float));
   return a;
 }
@@ -159,93 +170,3 @@ void kv4_launch_attention(hipStream_t s, int32_t dtype, int head_dim, const Kv4P
 }
 
 }  // namespace
-
-extern "C" {
-
-size_t ll_kv4_pool_bytes(const ll_kv4_cache* cache) {
-  Kv4Pool p;
-  return kv4_check_cache("ll_kv4_pool_bytes", cache, false, &p) == LL_OK ? 2 * (p.codes + p.params) : 0;
-}
-
-int ll_kv4_write(const ll_kv4_cache* cache, const ll_kv4_rows* rows, int32_t dtype, const ll_kv4_view* k, const ll_kv4_view* v,
-                 void* hip_stream) {
-  const char* who = "ll_kv4_write";
-  Kv4Pool p;
-  Kv4Rows r;
-  Kv4View kk, vv;
-  int rc;
-  if ((rc = kv4_check_cache(who, cache, true, &p)) != LL_OK || (rc = kv4_check_rows(who, rows, true, &r)) != LL_OK ||
-      (rc = kv4_check_type(who, dtype)) != LL_OK) return rc;
-  if (r.n_seqs == 0 || r.n_rows == 0) return LL_OK;
-  if ((rc = kv4_check_view(who, "k", k, rows, p.kv_heads, cache->head_dim, false, &kk)) != LL_OK ||
-      (rc = kv4_check_view(who, "v", v, rows, p.kv_heads, cache->head_dim, false, &vv)) != LL_OK) return rc;
-  kv4_launch_write(static_cast<hipStream_t>(hip_stream), dtype, cache->head_dim, p, r, kk, vv);
-  HIPCHK(hipGetLastError());
-  return LL_OK;
-}
-
-int ll_kv4_read(const ll_kv4_cache* cache, const ll_kv4_rows* rows, int32_t dtype, const ll_kv4_view* k, const ll_kv4_view* v,
-                void* hip_stream) {
-  const char* who = "ll_kv4_read";
-  Kv4Pool p;
-  Kv4Rows r;
-  Kv4View kk, vv;
-  int rc;
-  if ((rc = kv4_check_cache(who, cache, true, &p)) != LL_OK || (rc = kv4_check_rows(who, rows, true, &r)) != LL_OK ||
-      (rc = kv4_check_type(who, dtype)) != LL_OK) return rc;
-  if (r.n_seqs == 0 || r.n_rows == 0) return LL_OK;
-  if ((rc = kv4_check_view(who, "k", k, rows, p.kv_heads, cache->head_dim, true, &kk)) != LL_OK ||
-      (rc = kv4_check_view(who, "v", v, rows, p.kv_heads, cache->head_dim, true, &vv)) != LL_OK) return rc;
-  kv4_dispatch(dtype, cache->head_dim, [&](auto t, auto hd) {
-    kv4_row_blocks(p, r, cache->head_dim, [&](auto n, dim3 grid, dim3 threads) {
-      hipLaunchKernelGGL((kv4_read_kernel<decltype(t), decltype(hd)::value, decltype(n)::value>), grid, threads, 0,
-                         static_cast<hipStream_t>(hip_stream), p, r, kk, vv);
-    });
-  });
-  HIPCHK(hipGetLastError());
-  return LL_OK;
-}
-
-size_t ll_kv4_attention_workspace_bytes(const ll_kv4_cache* cache, const ll_kv4_rows* rows, int32_t n_heads) {
-  Kv4Pool p;
-  Kv4Rows r;
-  if (kv4_check_cache("ll_kv4_attention_workspace_bytes", cache, false, &p) != LL_OK ||
-      kv4_check_rows("ll_kv4_attention_workspace_bytes", rows, false, &r) != LL_OK || n_heads < 1 || n_heads % p.kv_heads) return 0;
-  return kv4_plan(p, r, rows->max_len, cache->head_dim, n_heads).bytes;
-}
-
-int ll_kv4_attention(const ll_kv4_cache* cache, const ll_kv4_rows* rows, int32_t dtype, int32_t n_heads, float scale,
-                     const ll_kv4_view* q, const ll_kv4_view* k, const ll_kv4_view* v, const ll_kv4_view* out, void* workspace,
-                     size_t workspace_bytes, void* hip_stream) {
-  const char* who = "ll_kv4_attention";
-  Kv4Pool p;
-  Kv4Rows r;
-  Kv4View qq, kk, vv, oo;
-  int rc;
-  if ((rc = kv4_check_cache(who, cache, true, &p)) != LL_OK || (rc = kv4_check_rows(who, rows, true, &r)) != LL_OK ||
-      (rc = kv4_check_type(who, dtype)) != LL_OK) return rc;
-  if (n_heads < 1 || n_heads > kKv4MaxHeads || n_heads % p.kv_heads)
-    return fail(LL_E_BAD_CONFIG, "%s: n_heads = %d, need a multiple of n_kv_heads = %d up to %d", who, n_heads, p.kv_heads, kKv4MaxHeads);
-  if (!(scale >= 0.f) || !(scale < INFINITY)) return fail(LL_E_BAD_ARG, "%s: scale = %g, need a finite value >= 0", who, (double)scale);
-  if (!k != !v) return fail(LL_E_BAD_ARG, "%s: k and v come together", who);
-  if (r.n_seqs == 0 || r.n_rows == 0) return LL_OK;
-  if ((rc = kv4_check_view(who, "q", q, rows, n_heads, cache->head_dim, false, &qq)) != LL_OK ||
-      (rc = kv4_check_view(who, "out", out, rows, n_heads, cache->head_dim, true, &oo)) != LL_OK) return rc;
-  if (k && ((rc = kv4_check_view(who, "k", k, rows, p.kv_heads, cache->head_dim, false, &kk)) != LL_OK ||
-            (rc = kv4_check_view(who, "v", v, rows, p.kv_heads, cache->head_dim, false, &vv)) != LL_OK)) return rc;
-  const Kv4Plan a = kv4_plan(p, r, rows->max_len, cache->head_dim, n_heads);
-  if (a.works * a.splits >= 1 << 24)
-    return fail(LL_E_BAD_ARG, "%s: %lld workgroups, a launch holds %d", who, (long long)(a.works * a.splits), (1 << 24) - 1);
-  if (workspace_bytes < a.bytes || (a.bytes && !workspace))
-    return fail(LL_E_WORKSPACE, "%s: workspace has %zu bytes, %zu needed", who, workspace_bytes, a.bytes);
-  if (a.bytes && reinterpret_cast<uintptr_t>(workspace) % kAlign)
-    return fail(LL_E_WORKSPACE, "%s: workspace must be %zu-byte aligned", who, kAlign);
-  const hipStream_t s = static_cast<hipStream_t>(hip_stream);
-  if (scale == 0.f) scale = 1.0f / sqrtf((float)cache->head_dim);
-  kv4_launch_attention(s, dtype, cache->head_dim, p, r, n_heads, scale, qq, k ? &kk : nullptr, k ? &vv : nullptr, oo, a,
-                       static_cast<float*>(workspace));
-  HIPCHK(hipGetLastError());
-  return LL_OK;
-}
-
-}  // extern "C"

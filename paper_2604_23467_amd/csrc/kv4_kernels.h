@@ -29,6 +29,7 @@ typedef u16 u16x8 __attribute__((ext_vector_type(8)));
 struct Kv4Pool {
   char* base;
   size_t codes, params;      // bytes of a codes region and of a parameters region, padding included
+  size_t layer;              // bytes from one layer's pool to the next, for calls on several layers
   int kv_heads, pool_rows, page_tokens;
   u32 magic;                 // position / page_tokens = (2 u magic) >> 32 >> shift for 0 <= u < 2^31
   int shift;
@@ -38,6 +39,7 @@ struct Kv4Pool {
 struct Kv4Rows {
   const int *row_start, *len, *table;
   const int* active;         // optional: 0 = the sequence has no positions
+  const int* order;          // optional: sequences in the order in which attention's workgroups take them
   int len_add;               // added to len[b]
   int n_seqs, max_rows, n_rows, table_stride;
 };
@@ -46,6 +48,8 @@ struct Kv4View {
   void* data;
   long row_stride, head_stride;
   int wide;                  // rows of every head can be read and written 16 bytes at a time
+  long layer_stride;         // from one layer to the next
+  int frag_k, frag_tb;       // frag_tb > 0: rows of frag_k elements in the projections' operand order (act_offset)
 };
 
 template <int HD>
@@ -156,8 +160,14 @@ __device__ __forceinline__ u16x8 kv4_load8(const Kv4View& t, int row, int head, 
   for (int i = 0; i < 8; ++i) v[i] = *as_global(p + i);
   return v;
 }
+template <int HD>
+__device__ __forceinline__ u16* kv4_element(const Kv4View& t, int row, int head, int e) {      // of an output
+  if (t.frag_tb) return (u16*)t.data + act_offset(row, head * HD + e, t.frag_k, t.frag_tb);
+  return (u16*)t.data + row * t.row_stride + (head * t.head_stride + e);
+}
+template <int HD>
 __device__ __forceinline__ void kv4_store8(const Kv4View& t, int row, int head, int e, u16x8 v) {
-  u16* p = (u16*)t.data + row * t.row_stride + (head * t.head_stride + e);
+  u16* p = kv4_element<HD>(t, row, head, e);
   if (t.wide) {
     *as_global(reinterpret_cast<u16x8*>(p)) = v;
   } else {
@@ -239,18 +249,20 @@ __device__ __forceinline__ u32 kv4_quantise(const float (&x)[8], u32& param) {
   return four(c[0], c[1], c[2], c[3]) | four(c[4], c[5], c[6], c[7]) << 16;
 }
 
-// Rows of k and v into the cache.  A thread takes 8 elements of N consecutive rows, four threads a group.  grid = (blocks of N
+// Rows of k and v into the cache, of several layers at once where grid.z = 2 x layers.  A thread takes 8 elements of N consecutive rows, four threads a group.  grid = (blocks of N
 // rows, parts of a row's kv_heads HD / 8 threads, keys and values).  The cache has a head's rows side by side, so the rows of a block share
 // lines of it: written one by one from different XCDs, a line of parameters (8 rows) would leave eight L2s in parts.
 template <class T, int HD, int N>
 __global__ __launch_bounds__(256) void kv4_write_kernel(Kv4Pool p, Kv4Rows r, Kv4View k, Kv4View v) {
   constexpr int UPR = HD / 8;
-  const int i0 = blockIdx.x * N, unit = blockIdx.y * blockDim.x + threadIdx.x, which = blockIdx.z;
+  const int i0 = blockIdx.x * N, unit = blockIdx.y * blockDim.x + threadIdx.x, which = blockIdx.z & 1;
   const int head = unit / UPR, oct = unit % UPR;
   int row[N];
   kv4_places<N>(p, r, i0, row);
   if (head >= p.kv_heads) return;
-  const Kv4View from = which ? v : k;
+  Kv4View from = which ? v : k;
+  from.data = (u16*)from.data + (blockIdx.z >> 1) * from.layer_stride;
+  p.base += (blockIdx.z >> 1) * p.layer;
   u16x8 in[N];
 #pragma unroll
   for (int n = 0; n < N; ++n)
@@ -297,7 +309,7 @@ __global__ __launch_bounds__(256) void kv4_read_kernel(Kv4Pool p, Kv4Rows r, Kv4
     u16x8 out;
 #pragma unroll
     for (int i = 0; i < 8; ++i) out[i] = row[n] < 0 ? (u16)0 : T::store(kv4_value(w[n], i, sc, mid));
-    kv4_store8(to, i0 + n, head, oct * 8, out);
+    kv4_store8<HD>(to, i0 + n, head, oct * 8, out);
   }
 }
 
@@ -372,14 +384,14 @@ __device__ __forceinline__ f4 kv4_mfma(h8 a, h8 b, f4 c) { return __builtin_amdg
 struct Kv4Work {
   int b, rb, head, split;
 };
-__device__ __forceinline__ Kv4Work kv4_work(int id, int splits, int kv_heads, int row_blocks) {
+__device__ __forceinline__ Kv4Work kv4_work(const Kv4Rows& r, int id, int splits, int kv_heads, int row_blocks) {
   Kv4Work w;
   w.split = id % splits;
   id /= splits;
   w.head = id % kv_heads;
   id /= kv_heads;
   w.rb = id % row_blocks;
-  w.b = id / row_blocks;
+  w.b = r.order ? kv4_scalar(r.order + id / row_blocks) : id / row_blocks;
   return w;
 }
 // Tiles of a share when `tiles` of them are dealt to `splits` workgroups: whole rounds of the waves
@@ -570,7 +582,7 @@ __device__ __forceinline__ int kv4_key(int i, int h) { return (i & 3) + 4 * h + 
 // groups that are NaN, must not meet a weight of zero: their parameters become zero.  Both are rare and found for the whole wave
 // at once: a sum of all middles is NaN if one is.
 template <int HD>
-__device__ __forceinline__ h8 kv4_middles(Kv4Tile<HD>& t, u32 there, int c, int h) {
+__device__ __forceinline__ h8 kv4_middles(Kv4Tile<HD>& t, u32 there, int c, int h, u32 mid_row, u32 one_row) {
   u32 marks = 0;
   h2 all = kv4_h2(t.vp[0]);
 #pragma unroll
@@ -585,12 +597,14 @@ __device__ __forceinline__ h8 kv4_middles(Kv4Tile<HD>& t, u32 there, int c, int 
     }
   }
   u32x4 w;
-  const u32 fill = c == 1 ? 0x3c003c00u : 0u;
 #pragma unroll
-  for (int a = 0; a < 4; ++a) w[a] = (c & 3) == 0 ? kv4_hi16(t.vp[2 * a], t.vp[2 * a + 1]) : fill;
-  if (marks && (c & 3) == 2) {
+  for (int a = 0; a < 4; ++a) w[a] = (kv4_hi16(t.vp[2 * a], t.vp[2 * a + 1]) & mid_row) | one_row;
+  if (__any(marks)) {
 #pragma unroll
-    for (int a = 0; a < 4; ++a) w[a] = (marks >> (2 * a) & 1 ? 0x3c00u : 0u) | (marks >> (2 * a + 1) & 1 ? 0x3c000000u : 0u);
+    for (int a = 0; a < 4; ++a) {
+      const u32 mark = (marks >> (2 * a) & 1 ? 0x3c00u : 0u) | (marks >> (2 * a + 1) & 1 ? 0x3c000000u : 0u);
+      w[a] = (c & 3) == 2 ? mark : w[a];
+    }
   }
   return __builtin_bit_cast(h8, w);
 }
@@ -627,7 +641,7 @@ __global__ __launch_bounds__(256, 3) void kv4_attn_few_kernel(Kv4Pool p, Kv4Rows
   __shared__ __attribute__((aligned(16))) u32 s_rows[P16 ? 1 : KV4_WAVES][KV4_TILE];
   __shared__ float s_m[KV4_WAVES][16];
   __shared__ __attribute__((aligned(16))) u32 s_new[2][HD / 8], s_newp[2][HD / 32];
-  const Kv4Work w = kv4_work(blockIdx.x, splits, p.kv_heads, row_blocks);
+  const Kv4Work w = kv4_work(r, blockIdx.x, splits, p.kv_heads, row_blocks);
   const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, h = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const Kv4Seq s = kv4_seq(r, w.b);
@@ -727,6 +741,7 @@ __global__ __launch_bounds__(256, 3) void kv4_attn_few_kernel(Kv4Pool p, Kv4Rows
   // Loads of a wave land in the order in which they were issued: keys and values of a tile, then those of the next.  A wait
   // leaves what is younger than its half of a tile in flight, and a half is fetched anew once its reads have arrived.
   const Kv4Bits bits;
+  const u32 mid_row = (c & 3) == 0 ? ~0u : 0u, one_row = c == 1 ? 0x3c003c00u : 0u;
   Kv4Tile<HD> tile;
   for (int slot = 0; t < t1; t += KV4_WAVES, slot ^= 1) {
     const int u0 = t * KV4_TILE;
@@ -807,7 +822,7 @@ __global__ __launch_bounds__(256, 3) void kv4_attn_few_kernel(Kv4Pool p, Kv4Rows
     __builtin_amdgcn_sched_barrier(0);
     ring.fetch_values(slot, where);
     __builtin_amdgcn_sched_barrier(0);
-    add(NE, kv4_middles<HD>(tile, has, c, h));
+    add(NE, kv4_middles<HD>(tile, has, c, h, mid_row, one_row));
     h8 op[4];
     kv4_values<HD, 0>(tile, bits, op);
 #pragma unroll
@@ -867,7 +882,7 @@ __global__ __launch_bounds__(256, 3) void kv4_attn_few_kernel(Kv4Pool p, Kv4Rows
       u16x8 v;
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = T::store(out[row][oct * 8 + e]);
-      kv4_store8(o, s.first + jj, w.head * share_heads + ff - jj * share_heads, oct * 8, v);
+      kv4_store8<HD>(o, s.first + jj, w.head * share_heads + ff - jj * share_heads, oct * 8, v);
     }
   } else {
     float* to = part + (size_t)blockIdx.x * 16 * (HD + 2);
@@ -930,7 +945,7 @@ __global__ __launch_bounds__(256, 2) void kv4_attn_many_kernel(Kv4Pool p, Kv4Row
   __shared__ __attribute__((aligned(16))) h8 s_frag[KV4_WAVES][Op::FRAGS][64];
   __shared__ __attribute__((aligned(16))) u32 s_rows[P16 ? 1 : KV4_WAVES][KV4_TILE];
   __shared__ u32 s_has[KV4_WAVES];
-  Kv4Work w = kv4_work(blockIdx.x, splits, p.kv_heads, row_blocks);
+  Kv4Work w = kv4_work(r, blockIdx.x, splits, p.kv_heads, row_blocks);
   w.rb = row_blocks - 1 - w.rb;                                            // the longest first
   const int tid = threadIdx.x, lane = tid & 63, c = lane & 31, h = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -998,6 +1013,7 @@ __global__ __launch_bounds__(256, 2) void kv4_attn_many_kernel(Kv4Pool p, Kv4Row
     }
   };
   const Kv4Bits bits;
+  const u32 mid_row = (c & 3) == 0 ? ~0u : 0u, one_row = (c & 3) == 1 ? 0x3c003c00u : 0u;
   // the wave's 32 keys as fragments: K's KS, their middles, then for either half of the keys V's NE and theirs
   auto produce = [&]() {
     h8(*out)[64] = s_frag[wave];
@@ -1036,8 +1052,15 @@ __global__ __launch_bounds__(256, 2) void kv4_attn_many_kernel(Kv4Pool p, Kv4Row
         bits.unpack(raw.v[n] | raw.v[n + 1] << 16, d);
 #pragma unroll
         for (int i = 0; i < NE; ++i) w4[i][a] = kv4_u32(d[i] * step);
-        const u32 mark = (marks >> n & 1 ? 0x3c00u : 0u) | (marks >> (n + 1) & 1 ? 0x3c000000u : 0u);
-        mids[a] = (c & 3) == 0 ? kv4_hi16(raw.vp[n], raw.vp[n + 1]) : (c & 3) == 1 ? 0x3c003c00u : (c & 3) == 2 ? mark : 0u;
+        mids[a] = (kv4_hi16(raw.vp[n], raw.vp[n + 1]) & mid_row) | one_row;
+      }
+      if (__any(marks)) {
+#pragma unroll
+        for (int a = 0; a < 4; ++a) {
+          const int n = 8 * t + 2 * a;
+          const u32 mark = (marks >> n & 1 ? 0x3c00u : 0u) | (marks >> (n + 1) & 1 ? 0x3c000000u : 0u);
+          mids[a] = (c & 3) == 2 ? mark : mids[a];
+        }
       }
 #pragma unroll
       for (int i = 0; i < NE; ++i) out[KS + 1 + t * (NE + 1) + i][lane] = __builtin_bit_cast(h8, w4[i]);
@@ -1170,7 +1193,7 @@ __global__ __launch_bounds__(256, 2) void kv4_attn_many_kernel(Kv4Pool p, Kv4Row
         u16x8 v;
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = T::store(y[8 * n + i]);
-        kv4_store8(o, s.first + j, qhead, e0 + 8 * n, v);
+        kv4_store8<HD>(o, s.first + j, qhead, e0 + 8 * n, v);
       } else {
         *reinterpret_cast<f4*>(to + at_row * HD + e0 + 8 * n) = f4{y[8 * n], y[8 * n + 1], y[8 * n + 2], y[8 * n + 3]};
         *reinterpret_cast<f4*>(to + at_row * HD + e0 + 8 * n + 4) = f4{y[8 * n + 4], y[8 * n + 5], y[8 * n + 6], y[8 * n + 7]};
@@ -1190,7 +1213,7 @@ __global__ __launch_bounds__(256) void kv4_join_kernel(Kv4Pool p, Kv4Rows r, Kv4
                                                        const float* part) {
   typedef float vec __attribute__((ext_vector_type(HD / 64)));
   constexpr size_t PART = ROWS * (HD + 2);
-  Kv4Work w = kv4_work(blockIdx.x, 1, p.kv_heads, row_blocks);
+  Kv4Work w = kv4_work(r, blockIdx.x, 1, p.kv_heads, row_blocks);
   if (ROWS > KV4_FEW_ROWS) w.rb = row_blocks - 1 - w.rb;
   const Kv4Seq s = kv4_seq(r, w.b);
   const int share_heads = heads / p.kv_heads, rows = min(s.rows, r.max_rows) * share_heads;
@@ -1219,7 +1242,7 @@ __global__ __launch_bounds__(256) void kv4_join_kernel(Kv4Pool p, Kv4Rows r, Kv4
       if (k + i < n) a += v[i] * __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, weight), k + i));
   }
   const int j = f / share_heads;
-  u16* to = (u16*)o.data + (s.first + j) * o.row_stride + (w.head * share_heads + f - j * share_heads) * o.head_stride + lane * (HD / 64);
+  u16* to = kv4_element<HD>(o, s.first + j, w.head * share_heads + f - j * share_heads, lane * (HD / 64));
 #pragma unroll
   for (int i = 0; i < HD / 64; ++i) to[i] = T::store(a[i] * inv);
 }

@@ -87,6 +87,12 @@ int num_cus() {
   return g_num_cus;
 }
 
+}  // namespace
+
+#include "kv4_host.h"
+
+namespace {
+
 bool config_ok(const ll_config* c, const char** why) {
   const char* w = nullptr;
   if (!c) w = "null config";
@@ -1316,22 +1322,40 @@ int run_decode_steps(Instance* I, int k) {
 // ---- batched lock-step decoding over a paged KV cache (batch_kernels.h) ----
 struct BatchLayout {
   size_t kv, page_table, state, dstate, logits, total;
-  size_t kv_layer_halves;     // halves per layer per K or V pool
+  size_t kv_layer_halves;     // halves per layer per K or V pool (16 bits)
+  size_t kv_bytes;            // all layers' pools
+  size_t fresh, part;         // 4 bits: a step's keys and values before they are quantised; shares of attention's keys
+  Kv4Pool kv4;                // 4 bits: the first layer's pool, but for its address
+  Kv4Plan plan;               // 4 bits: how a step's attention is cut into workgroups
   int pool_rows, pt_stride;
 };
 
-BatchLayout make_batch_layout(const ll_config& c, int page_tokens, int n_pages) {
+BatchLayout make_batch_layout(const ll_config& c, int page_tokens, int n_pages, int kv_bits, int rows) {
   BatchLayout B{};
   B.pool_rows = page_tokens * n_pages;
   B.pt_stride = (c.max_seq + page_tokens - 1) / page_tokens;
   B.kv_layer_halves = (size_t)c.n_heads * B.pool_rows * c.head_dim;
   size_t off = 0;
   auto take = [&](size_t bytes) { size_t o = off; off = align_up(off + bytes); return o; };
-  B.kv = take((size_t)c.n_layers * 2 * B.kv_layer_halves * 2);
+  B.kv_bytes = (size_t)c.n_layers * 2 * B.kv_layer_halves * 2;
+  if (kv_bits == 4) {
+    const ll_kv4_cache shape{nullptr, 0, c.n_heads, c.head_dim, page_tokens, n_pages};
+    (void)kv4_check_cache("ll_batch_open_kv", &shape, false, &B.kv4);       // (checked where the batch is opened)
+    B.kv4.layer = 2 * (B.kv4.codes + B.kv4.params);
+    B.kv_bytes = c.n_layers * B.kv4.layer;
+    Kv4Rows r{};
+    r.n_seqs = r.n_rows = rows; r.max_rows = 1; r.table_stride = B.pt_stride;
+    B.plan = kv4_plan(B.kv4, r, c.max_seq, c.head_dim, c.n_heads);
+  }
+  B.kv = take(B.kv_bytes);
   B.page_table = take((size_t)BT_MAX_BATCH * B.pt_stride * 4);
   B.state = take(sizeof(BatchState));
   B.dstate = take(sizeof(DevState));
   B.logits = take((size_t)BT_MAX_BATCH * c.vocab * 4);
+  if (kv_bits == 4) {
+    B.fresh = take((size_t)2 * BT_MAX_BATCH * c.d_model * 2);
+    B.part = take(B.plan.bytes);
+  }
   B.total = off;
   return B;
 }
@@ -1340,6 +1364,7 @@ struct Batch {
   BatchLayout L;
   char* pool = nullptr;
   int max_batch = 0, page_tokens = 0, n_pages = 0;
+  int kv_bits = 16;                            // of the pool's elements: 16 or 4
   int rows = 16;                               // rows of a step: 16 up to 16 slots, else 32
   std::vector<int> free_pages;                 // page 0 is never handed out: free slots write there
   std::vector<std::vector<int>> pages;         // pages of every slot, in order
@@ -1353,7 +1378,13 @@ struct Batch {
   template <typename T> T* at(size_t off) const { return reinterpret_cast<T*>(pool + off); }
   half_t* kpool(int layer) const { return at<half_t>(L.kv) + (size_t)layer * 2 * L.kv_layer_halves; }
   half_t* vpool(int layer) const { return kpool(layer) + L.kv_layer_halves; }
+  Kv4Pool kv4(int layer) const {
+    Kv4Pool p = L.kv4;
+    p.base = pool + L.kv + (size_t)layer * L.kv4.layer;
+    return p;
+  }
 };
+int batch_rows(int max_batch) { return max_batch <= 16 ? 16 : 32; }
 
 void destroy_batch(Batch* B) {
   if (!B) return;
@@ -1390,13 +1421,28 @@ void enqueue_batch_step(Instance* I, hipStream_t s) {
     a.ss_in = ss_attn; a.ss_parts = l == 0 ? 1 : parts;
     a.row_pos = bs->pos; a.page_table = table; a.pt_stride = B->L.pt_stride; a.page_tokens = B->page_tokens;
     a.Wf = I->wfrag(l, I->L.wf_qkv);
+    half_t* fresh = B->at<half_t>(B->L.fresh);       // 4 bits: keys, then values, [head][row of the step][head_dim]
+    const size_t fresh_v = (size_t)BT_MAX_BATCH * d;
+    if (B->kv_bits == 4) {
+      a.page_table = nullptr; a.rows_apart = 1; a.max_seq = Mb;
+      a.kc = fresh; a.vc = fresh + fresh_v;
+    }
     launch_skinny<SK_QKV>(s, P, a, Mb);
     dim3 agrid(c.n_heads, Mb);
     auto attn = [&](auto kernel, int threads) {
       hipLaunchKernelGGL(kernel, agrid, dim3(threads), (size_t)B->L.pt_stride * 4, s, Qh, B->kpool(l), B->vpool(l), bs,
                          table, B->L.pt_stride, B->page_tokens, Oh, d, B->L.pool_rows, tb);
     };
-    if (c.head_dim == 128) tb == 1 ? attn(bt_attn_kernel<128, BT_ATTN_THREADS(1)>, BT_ATTN_THREADS(1))
+    if (B->kv_bits == 4) {                           // quantises the new rows into their pages and attends, in one launch
+      Kv4Rows r{};
+      r.len = bs->pos; r.len_add = 1; r.active = bs->active; r.order = bs->order; r.table = table;
+      r.n_seqs = r.n_rows = Mb; r.max_rows = 1; r.table_stride = B->L.pt_stride;
+      const Kv4View q{Qh, d, c.head_dim, 1, 0, 0, 0}, k{fresh, c.head_dim, (long)Mb * c.head_dim, 1, 0, 0, 0},
+          v{fresh + fresh_v, c.head_dim, (long)Mb * c.head_dim, 1, 0, 0, 0}, o{Oh, 0, 0, 1, 0, d, tb};
+      kv4_launch_attention(s, LL_F16, c.head_dim, B->kv4(l), r, c.n_heads, 1.0f / sqrtf((float)c.head_dim), q, &k, &v, o, B->L.plan,
+                           B->at<float>(B->L.part));
+      a.rows_apart = 0;
+    } else if (c.head_dim == 128) tb == 1 ? attn(bt_attn_kernel<128, BT_ATTN_THREADS(1)>, BT_ATTN_THREADS(1))
                                      : attn(bt_attn_kernel<128, BT_ATTN_THREADS(2)>, BT_ATTN_THREADS(2));
     else tb == 1 ? attn(bt_attn_kernel<64, BT_ATTN_THREADS(1)>, BT_ATTN_THREADS(1))
                  : attn(bt_attn_kernel<64, BT_ATTN_THREADS(2)>, BT_ATTN_THREADS(2));
@@ -1879,12 +1925,21 @@ int32_t ll_decode_step(void) { return ll_decode_n(1, nullptr); }
 
 /* ---- batched lock-step decoding over a paged KV cache ---- */
 
-size_t ll_batch_pool_bytes(int32_t page_tokens, int32_t n_pages) {
-  if (!g || page_tokens < 1 || n_pages < 2) return 0;
-  return make_batch_layout(g->cfg, page_tokens, n_pages).total;
+size_t ll_batch_pool_bytes(int32_t page_tokens, int32_t n_pages) { return ll_batch_pool_bytes_kv(page_tokens, n_pages, 16); }
+
+// (a step's 32 rows: the larger of the two forms in what it needs besides)
+size_t ll_batch_pool_bytes_kv(int32_t page_tokens, int32_t n_pages, int32_t kv_bits) {
+  if (!g || page_tokens < 1 || n_pages < 2 || (kv_bits != 16 && kv_bits != 4)) return 0;
+  if (kv_bits == 4 && (int64_t)page_tokens * n_pages > kKv4MaxRows) return 0;
+  return std::max(make_batch_layout(g->cfg, page_tokens, n_pages, kv_bits, 16).total,
+                  make_batch_layout(g->cfg, page_tokens, n_pages, kv_bits, 32).total);
 }
 
 int ll_batch_open(int32_t max_batch, int32_t page_tokens, int32_t n_pages, void* pool, size_t pool_bytes) {
+  return ll_batch_open_kv(max_batch, page_tokens, n_pages, 16, pool, pool_bytes);
+}
+
+int ll_batch_open_kv(int32_t max_batch, int32_t page_tokens, int32_t n_pages, int32_t kv_bits, void* pool, size_t pool_bytes) {
   if (!g) return fail(LL_E_NOT_INIT, "ll_batch_open: not initialised");
   Instance* I = g;
   if (I->batch) return fail(LL_E_STATE, "ll_batch_open: already open; call ll_batch_close first");
@@ -1892,6 +1947,9 @@ int ll_batch_open(int32_t max_batch, int32_t page_tokens, int32_t n_pages, void*
     return fail(LL_E_BAD_ARG, "ll_batch_open: max_batch = %d outside [1, %d]", max_batch, BT_MAX_BATCH);
   if (page_tokens < 1 || n_pages < 2)
     return fail(LL_E_BAD_ARG, "ll_batch_open: need page_tokens >= 1 and n_pages >= 2 (page 0 is reserved)");
+  if (kv_bits != 16 && kv_bits != 4) return fail(LL_E_BAD_ARG, "ll_batch_open: kv_bits = %d, need 16 or 4", kv_bits);
+  if (kv_bits == 4 && (int64_t)page_tokens * n_pages > kKv4MaxRows)
+    return fail(LL_E_BAD_ARG, "ll_batch_open: a pool in 4 bits holds at most %d positions", kKv4MaxRows);
   if (!pool) return fail(LL_E_BAD_ARG, "ll_batch_open: null pool");
   const ll_config& c = I->cfg;
   const int per_wave = (((c.d_model + 31) >> 5) + SK_WAVES - 1) / SK_WAVES;
@@ -1900,8 +1958,8 @@ int ll_batch_open(int32_t max_batch, int32_t page_tokens, int32_t n_pages, void*
                                  "vocab %% 16 == 0 and head_dim 64 or 128");
   if (I->use_mega || I->per_length)
     return fail(LL_E_STATE, "ll_batch_open: available with the multi-kernel graph and eager modes only");
-  const BatchLayout BL = make_batch_layout(c, page_tokens, n_pages);
-  if (BL.pt_stride > 8192)
+  const BatchLayout BL = make_batch_layout(c, page_tokens, n_pages, kv_bits, batch_rows(max_batch));
+  if (kv_bits == 16 && BL.pt_stride > 8192)
     return fail(LL_E_BAD_ARG, "ll_batch_open: max_seq / page_tokens = %d pages per sequence, at most 8192 "
                               "(the attention kernel keeps a sequence's page list in LDS)", BL.pt_stride);
   if (pool_bytes < BL.total)
@@ -1913,7 +1971,8 @@ int ll_batch_open(int32_t max_batch, int32_t page_tokens, int32_t n_pages, void*
   B->L = BL;
   B->pool = static_cast<char*>(pool);
   B->max_batch = max_batch; B->page_tokens = page_tokens; B->n_pages = n_pages;
-  B->rows = max_batch <= 16 ? 16 : 32;
+  B->rows = batch_rows(max_batch);
+  B->kv_bits = kv_bits;
   for (int p = n_pages - 1; p >= 1; --p) B->free_pages.push_back(p);
   B->pages.resize(BT_MAX_BATCH);
   int rc = LL_OK;
@@ -1945,7 +2004,7 @@ int ll_batch_open(int32_t max_batch, int32_t page_tokens, int32_t n_pages, void*
     if (!ok(hipStreamSynchronize(I->stream), "batch init sync")) return bail(rc);
   }
   // page 0 must hold finite numbers: free slots attend nothing, but their K/V rows are written there
-  if (!ok(hipMemsetAsync(B->at<char>(BL.kv), 0, (size_t)c.n_layers * 2 * BL.kv_layer_halves * 2, I->stream),
+  if (!ok(hipMemsetAsync(B->at<char>(BL.kv), 0, BL.kv_bytes, I->stream),
           "hipMemset(pool)")) return bail(rc);
   if ((rc = push_batch_state(I, 0, BT_MAX_BATCH)) != LL_OK) return bail(rc);
   enqueue_batch_step(I, I->stream);                                         // warm-up on empty slots
@@ -2010,6 +2069,15 @@ int32_t ll_batch_add(const int32_t* tokens, int32_t n, int32_t* first_token) {
     int e = push_batch_state(I, slot, 1, I->state());
     if (e != LL_OK) return e;
     const ll_config& c = I->cfg;
+    if (B->kv_bits == 4) {                      // every layer's rows of the prompt, quantised
+      Kv4Rows r{};
+      r.len = B->at<BatchState>(B->L.state)->pos + slot; r.table = B->at<int>(B->L.page_table) + (size_t)slot * B->L.pt_stride;
+      r.n_seqs = 1; r.max_rows = r.n_rows = n; r.table_stride = B->L.pt_stride;
+      const Kv4View k{I->kcache(0), c.head_dim, (long)c.max_seq * c.head_dim, 1, 2 * (long)I->L.kv_layer_halves, 0, 0};
+      Kv4View v = k;
+      v.data = I->vcache(0);
+      kv4_launch_write(I->stream, LL_F16, c.head_dim, B->kv4(0), r, k, v, c.n_layers);
+    } else
     hipLaunchKernelGGL(bt_scatter_kernel, dim3(n, c.n_layers * 2), dim3(LL_WG), 0, I->stream, I->kcache(0),
                        I->L.kv_layer_halves, c.max_seq, B->kpool(0), B->L.kv_layer_halves, B->L.pool_rows,
                        B->at<int>(B->L.page_table), B->L.pt_stride, B->page_tokens, slot, c.n_heads, c.head_dim);
@@ -2116,6 +2184,56 @@ int ll_batch_dbg_get_logits(int32_t slot, float* host_out) {
   HIPCHK(hipStreamSynchronize(g->stream));
   HIPCHK(hipMemcpy(host_out, B->at<float>(B->L.logits) + (size_t)slot * g->cfg.vocab, (size_t)g->cfg.vocab * 4,
                    hipMemcpyDeviceToHost));
+  return LL_OK;
+}
+
+int ll_batch_dbg_get_kv(int32_t slot, int32_t layer, int32_t which, int32_t n_pos, float* host_out) {
+  if (!g) return fail(LL_E_NOT_INIT, "ll_batch_dbg_get_kv: not initialised");
+  Instance* I = g;
+  Batch* B = I->batch;
+  if (!B) return fail(LL_E_STATE, "ll_batch_dbg_get_kv: call ll_batch_open first");
+  const ll_config& c = I->cfg;
+  if (slot < 0 || slot >= B->max_batch || !B->h_state->active[slot] || layer < 0 || layer >= c.n_layers || (which != 0 && which != 1) ||
+      n_pos < 0 || n_pos > B->h_state->pos[slot] || !host_out)
+    return fail(LL_E_BAD_ARG, "ll_batch_dbg_get_kv: bad argument");
+  HIPCHK(hipStreamSynchronize(I->stream));
+  const int d = c.d_model;
+  std::vector<uint16_t> tmp;
+  auto put = [&](size_t pos, int head, int e, uint16_t bits) {
+    _Float16 v;
+    memcpy(&v, &bits, 2);
+    host_out[pos * d + (size_t)head * c.head_dim + e] = (float)v;
+  };
+  if (B->kv_bits == 4) {                        // read back by way of a prompt's activations, as many rows at a time as these hold
+    for (int p0 = 0; p0 < n_pos; p0 += I->L.mb_max) {
+      const int m = std::min(n_pos - p0, I->L.mb_max);
+      half_t* rows = reinterpret_cast<half_t*>(I->pf.X);
+      Kv4Rows r{};
+      r.len = B->at<BatchState>(B->L.state)->pos + slot; r.len_add = p0 + m - B->h_state->pos[slot];
+      r.table = B->at<int>(B->L.page_table) + (size_t)slot * B->L.pt_stride;
+      r.n_seqs = 1; r.max_rows = r.n_rows = m; r.table_stride = B->L.pt_stride;
+      const Kv4View k{rows, d, c.head_dim, 1, 0, 0, 0}, v{rows + (size_t)m * d, d, c.head_dim, 1, 0, 0, 0};
+      kv4_launch_read(I->stream, LL_F16, c.head_dim, B->kv4(layer), r, k, v);
+      HIPCHK(hipGetLastError());
+      HIPCHK(hipStreamSynchronize(I->stream));
+      tmp.resize((size_t)m * d);
+      HIPCHK(hipMemcpy(tmp.data(), (which ? v : k).data, tmp.size() * 2, hipMemcpyDeviceToHost));
+      for (int i = 0; i < m; ++i)
+        for (int x = 0; x < d; ++x) put(p0 + i, x / c.head_dim, x % c.head_dim, tmp[(size_t)i * d + x]);
+    }
+    return LL_OK;
+  }
+  tmp.resize((size_t)B->page_tokens * c.head_dim);
+  for (int p0 = 0, i = 0; p0 < n_pos; p0 += B->page_tokens, ++i) {
+    const int m = std::min(n_pos - p0, B->page_tokens);
+    for (int head = 0; head < c.n_heads; ++head) {
+      const half_t* src = (which ? B->vpool(layer) : B->kpool(layer)) +
+                          ((size_t)head * B->L.pool_rows + (size_t)B->pages[slot][i] * B->page_tokens) * c.head_dim;
+      HIPCHK(hipMemcpy(tmp.data(), src, (size_t)m * c.head_dim * 2, hipMemcpyDeviceToHost));
+      for (int j = 0; j < m; ++j)
+        for (int e = 0; e < c.head_dim; ++e) put(p0 + j, head, e, tmp[(size_t)j * c.head_dim + e]);
+    }
+  }
   return LL_OK;
 }
 
@@ -2486,4 +2604,4 @@ int ll_dbg_time_decode(int32_t k, float* ms_out) {
 
 }  // extern "C"
 
-#include "kv4_host.h"
+#include "kv4_api.h"

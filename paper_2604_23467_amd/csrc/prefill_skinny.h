@@ -74,6 +74,7 @@ struct SkinnyArgs {
   const int* row_pos;     // QKV: position of row r (null: st->pos + r)
   const int* page_table;  // QKV: [rows][pt_stride] first cache row of each page of row r's sequence (null: cache row = position)
   int pt_stride, page_tokens;
+  int rows_apart;         // QKV without a page table: cache row = row of the step, for a cache that takes its rows from there
   float* logits;          // LOGITS: [rows][N] fp32, normalised like QKV / GATEUP outputs
 };
 
@@ -82,7 +83,7 @@ __device__ __forceinline__ int sk_row_pos(const SkinnyArgs& a, int p0, int tok) 
   return a.row_pos ? a.row_pos[tok] : p0 + tok;
 }
 __device__ __forceinline__ int sk_cache_row(const SkinnyArgs& a, int tok, int pos) {
-  if (!a.page_table) return pos;
+  if (!a.page_table) return a.rows_apart ? tok : pos;
   const int pg = pos / a.page_tokens;
   return a.page_table[tok * a.pt_stride + pg] + (pos - pg * a.page_tokens);
 }

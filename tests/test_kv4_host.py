@@ -115,3 +115,11 @@ def test_definition_holds_what_it_promises():
     assert ((15 * smaller < span) | (eight != eight.round()))[s > 0].all()
     off = (ku.values(c, s, mid) - x.double()).abs().reshape(500, 4, 32)
     assert (off <= (s / 2 + mid.abs() * 2.0 ** -11 + 2.0 ** -25)[..., None]).all()
+
+
+def test_batch_calls_with_a_choice_of_bits_need_an_instance():
+    lib = b.load()
+    out = (C.c_float * 4)()
+    assert lib.ll_batch_pool_bytes_kv(16, 8, 4) == 0
+    assert lib.ll_batch_open_kv(4, 16, 8, 4, C.c_void_p(256), 1 << 20) == b.LL_E_NOT_INIT
+    assert lib.ll_batch_dbg_get_kv(0, 0, 0, 1, out) == b.LL_E_NOT_INIT
