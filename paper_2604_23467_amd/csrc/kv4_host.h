@@ -158,10 +158,16 @@ void kv4_launch_attention(hipStream_t s, int32_t dtype, int head_dim, const Kv4P
                            heads, a.splits, a.row_blocks, part);
       return;
     }
+    auto single = [&](auto kernel) {
+      hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, p, r, q, o, fresh ? *k : q, fresh ? *v : q, heads, scale, a.splits, part);
+    };
     auto go = [&](auto kernel) {
       hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, p, r, q, o, fresh ? *k : q, fresh ? *v : q, heads, scale, a.splits, a.row_blocks, part);
     };
-    if (p16) fresh ? go(kv4_attn_few_kernel<T, HD, true, true>) : go(kv4_attn_few_kernel<T, HD, true, false>);
+    if (r.max_rows == 1 && heads == p.kv_heads) {
+      if (p16) fresh ? single(kv4_attn_one_kernel<T, HD, true, true>) : single(kv4_attn_one_kernel<T, HD, true, false>);
+      else fresh ? single(kv4_attn_one_kernel<T, HD, false, true>) : single(kv4_attn_one_kernel<T, HD, false, false>);
+    } else if (p16) fresh ? go(kv4_attn_few_kernel<T, HD, true, true>) : go(kv4_attn_few_kernel<T, HD, true, false>);
     else fresh ? go(kv4_attn_few_kernel<T, HD, false, true>) : go(kv4_attn_few_kernel<T, HD, false, false>);
     if (a.splits > 1)
       hipLaunchKernelGGL((kv4_join_kernel<T, HD, KV4_FEW_ROWS>), dim3((unsigned)a.works, KV4_FEW_ROWS / 4), dim3(256), 0, s, p, r, o, heads,

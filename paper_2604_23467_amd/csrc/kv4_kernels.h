@@ -897,6 +897,286 @@ __global__ __launch_bounds__(256, 3) void kv4_attn_few_kernel(Kv4Pool p, Kv4Rows
   }
 }
 
+// all of a workgroup's waves, without waiting for loads in flight
+__device__ __forceinline__ void kv4_barrier() {
+  wait_lgkm_at_most<0>();
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// ---- one query row a key head ----
+//
+// A single row leaves fifteen of sixteen columns of the matrix instructions empty, and their operands cost the vector unit more
+// than the products themselves: a code takes 1.1 operations for the score (half words set into 1024 + c, as above, then two at
+// a time into v_dot2_f32_f16; what 1024 and 64 add up to is taken off in front, as the start of the sum) and 2.1 for the output
+// (c - 8, then a multiply-add from a half word to 32 bits).  HD / 32 lanes hold a key, a group of 32 elements each, so that a lane
+// has one step and one middle.  All of a wave's lanes share the running maximum; weights stay in 32 bits.
+#define KV4_ONE_STEPS 4          // keys of a lane in a trip
+
+template <class T, int HD, bool P16, bool NEW>
+__global__ __launch_bounds__(256, 3) void kv4_attn_one_kernel(Kv4Pool p, Kv4Rows r, Kv4View q, Kv4View o, Kv4View knew, Kv4View vnew,
+                                                              int heads, float scale, int splits, float* part) {
+  constexpr int U = KV4_ONE_STEPS, LPK = HD / 32, KPS = 64 / LPK, TRIP = U * KPS, NEXT = KV4_WAVES * TRIP;
+  __shared__ float s_acc[KV4_WAVES * 4][HD], s_part[KV4_WAVES * 4][LPK], s_m[KV4_WAVES], s_l[KV4_WAVES];
+  __shared__ __attribute__((aligned(16))) u32 s_new[2][HD / 8], s_newp[2][LPK];
+  const Kv4Work w = kv4_work(r, blockIdx.x, splits, p.kv_heads, 1);
+  const int tid = threadIdx.x, lane = tid & 63, g = lane % LPK;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const Kv4Seq s = kv4_seq(r, w.b);
+  if (s.rows < 1) return;
+  const int n_keys = max(s.len - s.rows + 1, 0);
+  const int tiles = (n_keys + KV4_TILE - 1) / KV4_TILE, share = kv4_share(tiles, splits);
+  const int t0 = w.split * share, end = min((t0 + share) * KV4_TILE, n_keys);
+  if (w.split > 0 && t0 >= tiles) return;
+  const int* table = r.table + (size_t)w.b * r.table_stride;
+
+  // pool rows of a trip's keys (or, with P16, of the first of every 16 keys); entries are requested a trip ahead
+  constexpr int PER = P16 ? KPS / 16 : 1, ENTRIES = U * PER;
+  auto page = [&](int u) { return (int)(__umulhi((u32)u << 1, p.magic) >> p.shift); };
+  auto look = [&](int k, u32 (&at)[ENTRIES]) {
+#pragma unroll
+    for (int i = 0; i < ENTRIES; ++i) {
+      const int u = P16 ? k + 16 * i : k + KPS * i + lane / LPK;
+      const int* e = table + min(page(u), r.table_stride - 1);
+      at[i] = P16 ? (u32)kv4_scalar(e) : (u32)*as_global(e);
+    }
+  };
+  auto place = [&](int k, const u32 (&at)[ENTRIES], int (&row)[ENTRIES]) {      // -1: none
+#pragma unroll
+    for (int i = 0; i < ENTRIES; ++i) {
+      const int u = P16 ? k + 16 * i : k + KPS * i + lane / LPK, pg = page(u);
+      row[i] = u < n_keys && pg < r.table_stride && at[i] <= (u32)(p.pool_rows - p.page_tokens) ? (int)(at[i] + (u - pg * p.page_tokens)) : -1;
+    }
+  };
+  const char *kc = kv4_codes<HD>(p, 0, w.head), *kp = kv4_params<HD>(p, 0, w.head);
+  const char *vc = kv4_codes<HD>(p, 1, w.head), *vp = kv4_params<HD>(p, 1, w.head);
+  auto fetch = [&](const char* codes, const char* params, const int (&row)[ENTRIES], u32x4 (&c)[U], u32 (&par)[U]) {
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      if (P16 && PER == 1) {                           // a scalar row, and a lane's place behind it
+        const u32 at = max(row[i], 0), x = lane / LPK;
+        c[i] = *as_global(reinterpret_cast<const u32x4*>(codes + (size_t)at * (HD / 2) + (x * (HD / 2) + g * 16)));
+        par[i] = *as_global(reinterpret_cast<const u32*>(params + (size_t)at * (HD / 8) + (x * (HD / 8) + g * 4)));
+      } else {
+        const int first = row[i * PER], last = row[i * PER + PER - 1];
+        const u32 at = P16 ? (u32)max(lane & 32 ? last : first, 0) + (lane / LPK & 15) : (u32)max(first, 0);
+        c[i] = *as_global(reinterpret_cast<const u32x4*>(codes + (size_t)(at * (HD / 2) + g * 16)));
+        par[i] = *as_global(reinterpret_cast<const u32*>(params + (size_t)(at * (HD / 8) + g * 4)));
+      }
+    }
+  };
+  // which of the lane's keys exist (a bit each)
+  auto exist = [&](int k, const int (&row)[ENTRIES]) {
+    u32 m = 0;
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const int first = row[i * PER], last = row[i * PER + PER - 1], at = PER == 2 && (lane & 32) ? last : first;
+      if (at >= 0 && k + KPS * i + lane / LPK < end) m |= 1u << i;
+    }
+    return m;
+  };
+  u32x4 kk[U], vv[U];
+  u32 kq[U], vq[U], at[ENTRIES];
+  u32 has = 0;
+  int k = t0 * KV4_TILE + wave * TRIP;
+  if (k < end) {
+    u32 now[ENTRIES];
+    int row[ENTRIES];
+    look(k, now);
+    look(k + NEXT, at);
+    place(k, now, row);
+    has = exist(k, row);
+    fetch(kc, kp, row, kk, kq);
+    fetch(vc, vp, row, vv, vq);
+  }
+
+  // The lane's group of the query, in the order in which codes unpack, scaled by a power of two to a largest element of
+  // 2^14 .. 2^15 (far from binary16's subnormal numbers, which the product may pass over)
+  h2 qf[16];
+  float qsum = 0.f, start = 0.f, qscale;
+  {
+    float x[32], top = 0.f;
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+      const u16x8 in = kv4_load8(q, s.first, w.head, g * 32 + n * 8);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        x[8 * n + i] = T::load(in[i]);
+        top = fmaxf(top, fabsf(x[8 * n + i]));
+      }
+    }
+    top = fmaxf(top, dpp_mov<0xB1>(top));
+    if (LPK == 4) top = fmaxf(top, dpp_mov<0x4E>(top));
+    const int e = top > 0.f && top < INFINITY ? ilogbf(top) - 14 : 0;
+#pragma unroll
+    for (int n = 0; n < 4; ++n)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const half_t a = (half_t)ldexpf(x[8 * n + i], -e), b = (half_t)ldexpf(x[8 * n + i + 4], -e);
+        qf[4 * n + i] = h2{a, b};
+        const float ab = (float)a + (float)b;
+        qsum += ab;
+        start -= ab * (i & 1 ? 72.f : 1032.f);
+      }
+    qscale = fmaxf(ldexpf(scale * 1.44269504088896340736f, e), 0x1p-126f);
+  }
+  const int pnew = NEW ? s.len - s.rows : -1;
+  const bool mine = NEW && pnew >= t0 * KV4_TILE && pnew < end;
+  if (mine) {
+    if (wave < 2 && lane < HD / 8) {
+      const u16x8 in = kv4_load8(wave ? vnew : knew, s.first, w.head, lane * 8);
+      float x[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = T::load(in[i]);
+      u32 param;
+      const u32 code = kv4_quantise(x, param);
+      s_new[wave][lane] = code;
+      s_newp[wave][lane >> 2] = param;
+      const int to = kv4_row(p, table, r.table_stride, pnew);
+      if (to >= 0) {
+        *(u32*)(kv4_codes<HD>(p, wave, w.head) + (size_t)to * (HD / 2) + lane * 4) = code;
+        if (lane % 4 == 0) *(u32*)(kv4_params<HD>(p, wave, w.head) + (size_t)to * (HD / 8) + lane) = param;
+      }
+    }
+    kv4_barrier();
+  }
+
+  const Kv4Bits bits;
+  float acc[32], sum_mid = 0.f, l = 0.f, m = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < 32; ++i) acc[i] = 0.f;
+  for (; k < end; k += NEXT) {
+    const bool more = k + NEXT < end;
+    int row[ENTRIES];
+    u32 has_next = 0;
+    if (more) {
+      place(k + NEXT, at, row);
+      has_next = exist(k + NEXT, row);
+      look(k + 2 * NEXT, at);
+    }
+    const bool fresh = mine && pnew >= k && pnew < k + TRIP;
+    const int fresh_step = (pnew - k) / KPS, fresh_lane = (pnew - k) % KPS;
+    if (fresh && lane / LPK == fresh_lane) {
+#pragma unroll
+      for (int i = 0; i < U; ++i)
+        if (i == fresh_step) {
+          kk[i] = *reinterpret_cast<const u32x4*>(&s_new[0][4 * g]);
+          kq[i] = s_newp[0][g];
+          vv[i] = *reinterpret_cast<const u32x4*>(&s_new[1][4 * g]);
+          vq[i] = s_newp[1][g];
+        }
+    }
+    float x[U];
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      float dot = start;
+#pragma unroll
+      for (int n = 0; n < 4; ++n) {
+        const u32 c = kk[i][n], y = c >> 8;
+        dot = __builtin_amdgcn_fdot2(kv4_h2((c & bits.low) | bits.k1024), qf[4 * n], dot, false);
+        dot = __builtin_amdgcn_fdot2(kv4_h2((c & bits.high) | bits.k64), qf[4 * n + 1], dot, false);
+        dot = __builtin_amdgcn_fdot2(kv4_h2((y & bits.low) | bits.k1024), qf[4 * n + 2], dot, false);
+        dot = __builtin_amdgcn_fdot2(kv4_h2((y & bits.high) | bits.k64), qf[4 * n + 3], dot, false);
+      }
+      const h2 par = kv4_h2(kq[i]);
+      float t = fmaf((float)par[0], dot, (float)par[1] * qsum);
+      t += dpp_mov<0xB1>(t);
+      if (LPK == 4) t += dpp_mov<0x4E>(t);
+      x[i] = t * qscale;
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    if (more) fetch(kc, kp, row, kk, kq);
+    if (__any(has != (1u << U) - 1)) {
+#pragma unroll
+      for (int i = 0; i < U; ++i)
+        if (!(has >> i & 1)) {                         // no weight, and nothing that a weight of zero could meet
+          x[i] = -INFINITY;
+          vq[i] = 0;
+        }
+    }
+    float top = x[0];
+#pragma unroll
+    for (int i = 1; i < U; ++i) top = fmaxf(top, x[i]);
+    if (LPK == 2) top = fmaxf(top, dpp_mov<0x4E>(top));
+    top = fmaxf(top, dpp_mov<0x124>(top));             // row_ror:4, row_ror:8: a row of 16 lanes
+    top = fmaxf(top, dpp_mov<0x128>(top));
+    top = fmaxf(kv4_max_over_quarters(top), m);
+    if (top > m) {                                     // the same for all lanes
+      const float corr = __builtin_amdgcn_exp2f(m - top);
+      m = top;
+      l *= corr;
+      sum_mid *= corr;
+#pragma unroll
+      for (int i = 0; i < 32; ++i) acc[i] *= corr;
+    }
+    const float base = m > -INFINITY ? m : 0.f;
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const float w1 = __builtin_amdgcn_exp2f(x[i] - base);
+      const h2 par = kv4_h2(vq[i]);
+      const float ws = w1 * (float)par[0];
+      l += w1;
+      sum_mid = fmaf(w1, (float)par[1], sum_mid);
+#pragma unroll
+      for (int n = 0; n < 4; ++n) {
+        h2 d[4];
+        bits.unpack(vv[i][n], d);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          acc[8 * n + e] = fmaf(ws, (float)d[e][0], acc[8 * n + e]);
+          acc[8 * n + e + 4] = fmaf(ws, (float)d[e][1], acc[8 * n + e + 4]);
+        }
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    if (more) fetch(vc, vp, row, vv, vq);
+    has = has_next;
+  }
+
+  // the lanes of a group within rows of 16 lanes, then the rows of all waves, meet
+  if (lane == 0) s_m[wave] = m;
+  __syncthreads();
+  float top = s_m[0];
+#pragma unroll
+  for (int i = 1; i < KV4_WAVES; ++i) top = fmaxf(top, s_m[i]);
+  const float weight = m > -INFINITY ? __builtin_amdgcn_exp2f(m - top) : 0.f;
+  auto row_sum = [&](float v) {
+    if (LPK == 2) v += dpp_mov<0x4E>(v);
+    v += dpp_mov<0x124>(v);
+    return v + dpp_mov<0x128>(v);
+  };
+#pragma unroll
+  for (int i = 0; i < 32; ++i) acc[i] = row_sum(acc[i] * weight);
+  sum_mid = row_sum(sum_mid * weight);
+  l = row_sum(l * weight);
+  l += __shfl_xor(l, 16);
+  l += __shfl_xor(l, 32);
+  if (lane == 0) s_l[wave] = l;
+  if ((lane & 15) < LPK) {
+    const int at_row = wave * 4 + (lane >> 4);
+    s_part[at_row][g] = sum_mid;
+#pragma unroll
+    for (int n = 0; n < 8; ++n)
+      *reinterpret_cast<f4*>(&s_acc[at_row][g * 32 + n * 4]) = f4{acc[4 * n], acc[4 * n + 1], acc[4 * n + 2], acc[4 * n + 3]};
+  }
+  __syncthreads();
+  l = 0.f;
+#pragma unroll
+  for (int i = 0; i < KV4_WAVES; ++i) l += s_l[i];
+  if (tid < HD) {
+    float v = 0.f;
+#pragma unroll
+    for (int i = 0; i < KV4_WAVES * 4; ++i) v += s_acc[i][tid] + s_part[i][tid / 32];
+    if (splits == 1) *kv4_element<HD>(o, s.first, w.head, tid) = T::store(l != 0.f ? v / l : 0.f);
+    else part[(size_t)blockIdx.x * KV4_FEW_ROWS * (HD + 2) + tid] = v;
+  }
+  if (splits > 1 && tid == 0) {
+    float* to = part + (size_t)blockIdx.x * KV4_FEW_ROWS * (HD + 2) + KV4_FEW_ROWS * HD;
+    to[0] = top;
+    to[KV4_FEW_ROWS] = l;
+  }
+}
+
 // ---- many query rows ----
 //
 // 128 query rows of one key head, 32 a wave.  Here the products count, and the 32x32x16 form has the higher rate; codes are
@@ -916,13 +1196,6 @@ __device__ __forceinline__ float kv4_max_over_halves(float v) {
   const auto r = __builtin_amdgcn_permlane32_swap(b, b, false, false);
   return fmaxf(__builtin_bit_cast(float, (u32)r[0]), __builtin_bit_cast(float, (u32)r[1]));
 }
-// all of a workgroup's waves, without waiting for loads in flight
-__device__ __forceinline__ void kv4_barrier() {
-  wait_lgkm_at_most<0>();
-  __builtin_amdgcn_s_barrier();
-  asm volatile("" ::: "memory");
-}
-
 template <int HD>
 struct Kv4Operands {
   static constexpr int KS = HD / 16, NE = HD / 32;            // products of a score; row blocks of elements
