@@ -409,15 +409,13 @@ struct Kv4Query {
   float scale;
 };
 template <class T, int HD>
-__device__ __forceinline__ void kv4_load_query(const Kv4View& v, bool there, int row, int head, int h, float scale, Kv4Query<HD>& out) {
+__device__ __forceinline__ void kv4_query(const u16x8 (&in)[HD / 32], float scale, Kv4Query<HD>& out) {
   float x[HD / 32][8], top = 0.f;
 #pragma unroll
   for (int s = 0; s < HD / 32; ++s) {
-    u16x8 in{};
-    if (there) in = kv4_load8(v, row, head, h * (HD / 4) + s * 8);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      x[s][i] = T::load(in[i]);
+      x[s][i] = T::load(in[s][i]);
       top = fmaxf(top, fabsf(x[s][i]));
     }
   }
@@ -655,6 +653,19 @@ __global__ __launch_bounds__(256, 3) void kv4_attn_few_kernel(Kv4Pool p, Kv4Rows
   if (w.split > 0 && t0 >= tiles) return;
   const int* table = r.table + (size_t)w.b * r.table_stride;
 
+  // requested in front of everything that waits for the page table
+  const int f = f0 + c, j = f / share_heads, qhead = w.head * share_heads + f - j * share_heads;
+  const bool there = f < rows;
+  const int limit = there ? s.len - s.rows + j : -1;                       // last position that the lane's query sees
+  u16x8 qin[HD / 32], nin{};
+#pragma unroll
+  for (int n = 0; n < HD / 32; ++n) {
+    qin[n] = u16x8{};
+    if (there) qin[n] = kv4_load8(q, s.first + j, qhead, h * (HD / 4) + n * 8);
+  }
+  if (NEW && wave < 2 && lane < HD / 8) nin = kv4_load8(wave ? vnew : knew, s.first, w.head, lane * 8);
+  __builtin_amdgcn_sched_barrier(0);
+
   // Pool rows of a tile: the page table's entries are requested a tile ahead of the tile's own loads.  place() then says where
   // the rows are, and which of the tile's keys have one (others: row 0).  Without P16 a lane looks after a key, and the rows go
   // through LDS.
@@ -706,18 +717,14 @@ __global__ __launch_bounds__(256, 3) void kv4_attn_few_kernel(Kv4Pool p, Kv4Rows
     __builtin_amdgcn_sched_barrier(0);
   }
 
-  const int f = f0 + c, j = f / share_heads, qhead = w.head * share_heads + f - j * share_heads;
-  const bool there = f < rows;
-  const int limit = there ? s.len - s.rows + j : -1;                       // last position that the lane's query sees
   Kv4Query<HD> query;
-  kv4_load_query<T, HD>(q, there, s.first + j, qhead, h, scale, query);
+  kv4_query<T, HD>(qin, scale, query);
   const int pnew = NEW ? s.len - s.rows : -1;
   if (NEW && pnew >= 0 && pnew / KV4_TILE >= t0 && pnew / KV4_TILE < t1) {
     if (wave < 2 && lane < HD / 8) {
-      const u16x8 in = kv4_load8(wave ? vnew : knew, s.first, w.head, lane * 8);
       float x[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = T::load(in[i]);
+      for (int i = 0; i < 8; ++i) x[i] = T::load(nin[i]);
       u32 param;
       const u32 code = kv4_quantise(x, param);
       s_new[wave][lane] = code;
@@ -911,10 +918,10 @@ __device__ __forceinline__ void kv4_barrier() {
 // a time into v_dot2_f32_f16; what 1024 and 64 add up to is taken off in front, as the start of the sum) and 2.1 for the output
 // (c - 8, then a multiply-add from a half word to 32 bits).  HD / 32 lanes hold a key, a group of 32 elements each, so that a lane
 // has one step and one middle.  All of a wave's lanes share the running maximum; weights stay in 32 bits.
-#define KV4_ONE_STEPS 4          // keys of a lane in a trip
+#define KV4_ONE_STEPS 2          // keys of a lane in a trip: 4 of them leave registers for three workgroups a CU only (77 -> 79 us)
 
 template <class T, int HD, bool P16, bool NEW>
-__global__ __launch_bounds__(256, 3) void kv4_attn_one_kernel(Kv4Pool p, Kv4Rows r, Kv4View q, Kv4View o, Kv4View knew, Kv4View vnew,
+__global__ __launch_bounds__(256, 4) void kv4_attn_one_kernel(Kv4Pool p, Kv4Rows r, Kv4View q, Kv4View o, Kv4View knew, Kv4View vnew,
                                                               int heads, float scale, int splits, float* part) {
   constexpr int U = KV4_ONE_STEPS, LPK = HD / 32, KPS = 64 / LPK, TRIP = U * KPS, NEXT = KV4_WAVES * TRIP;
   __shared__ float s_acc[KV4_WAVES * 4][HD], s_part[KV4_WAVES * 4][LPK], s_m[KV4_WAVES], s_l[KV4_WAVES];
@@ -929,6 +936,13 @@ __global__ __launch_bounds__(256, 3) void kv4_attn_one_kernel(Kv4Pool p, Kv4Rows
   const int t0 = w.split * share, end = min((t0 + share) * KV4_TILE, n_keys);
   if (w.split > 0 && t0 >= tiles) return;
   const int* table = r.table + (size_t)w.b * r.table_stride;
+
+  // requested in front of everything that waits for the page table
+  u16x8 qin[4], nin{};
+#pragma unroll
+  for (int n = 0; n < 4; ++n) qin[n] = kv4_load8(q, s.first, w.head, g * 32 + n * 8);
+  if (NEW && wave < 2 && lane < HD / 8) nin = kv4_load8(wave ? vnew : knew, s.first, w.head, lane * 8);
+  __builtin_amdgcn_sched_barrier(0);
 
   // pool rows of a trip's keys (or, with P16, of the first of every 16 keys); entries are requested a trip ahead
   constexpr int PER = P16 ? KPS / 16 : 1, ENTRIES = U * PER;
@@ -998,10 +1012,9 @@ __global__ __launch_bounds__(256, 3) void kv4_attn_one_kernel(Kv4Pool p, Kv4Rows
     float x[32], top = 0.f;
 #pragma unroll
     for (int n = 0; n < 4; ++n) {
-      const u16x8 in = kv4_load8(q, s.first, w.head, g * 32 + n * 8);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        x[8 * n + i] = T::load(in[i]);
+        x[8 * n + i] = T::load(qin[n][i]);
         top = fmaxf(top, fabsf(x[8 * n + i]));
       }
     }
@@ -1024,10 +1037,9 @@ __global__ __launch_bounds__(256, 3) void kv4_attn_one_kernel(Kv4Pool p, Kv4Rows
   const bool mine = NEW && pnew >= t0 * KV4_TILE && pnew < end;
   if (mine) {
     if (wave < 2 && lane < HD / 8) {
-      const u16x8 in = kv4_load8(wave ? vnew : knew, s.first, w.head, lane * 8);
       float x[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = T::load(in[i]);
+      for (int i = 0; i < 8; ++i) x[i] = T::load(nin[i]);
       u32 param;
       const u32 code = kv4_quantise(x, param);
       s_new[wave][lane] = code;
