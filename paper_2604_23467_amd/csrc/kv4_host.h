@@ -129,11 +129,11 @@ Kv4Plan kv4_plan(const Kv4Pool& p, const Kv4Rows& r, int max_len, int head_dim, 
   // Blocks of 128 rows where they, times the shares, leave no CU idle.  One sequence of 500 rows and 32 heads, 128 such
   // workgroups: 28.6 us, in blocks of 16 rows 21.2; six of up to 700 behind up to 2000, 1056 workgroups: 120, 160.
   const int64_t many = (rows + KV4_MANY_ROWS - 1) / KV4_MANY_ROWS * p.kv_heads * r.n_seqs;
-  a.many = rows > KV4_MANY_ROWS / 2 && many * shares >= num_cus();
+  a.many = rows > 64 && many * shares >= num_cus();
   const int block = a.many ? KV4_MANY_ROWS : KV4_FEW_ROWS;
   a.row_blocks = (int)((rows + block - 1) / block);
   a.works = (int64_t)a.row_blocks * p.kv_heads * r.n_seqs;
-  const int64_t want = (2 * num_cus() + a.works - 1) / std::max<int64_t>(a.works, 1);
+  const int64_t want = ((a.many ? 1 : 2) * num_cus() + a.works - 1) / std::max<int64_t>(a.works, 1);
   a.splits = (int)std::min<int64_t>(want, shares);
   if (a.splits > 1) a.bytes = align_up((size_t)a.works * a.splits * block * (head_dim + 2) * sizeof(float));
   return a;
@@ -150,7 +150,7 @@ void kv4_launch_attention(hipStream_t s, int32_t dtype, int head_dim, const Kv4P
     const bool p16 = p.page_tokens % 16 == 0;
     if (a.many) {
       auto go = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, p, r, q, o, heads, scale, a.splits, a.row_blocks, part);
+        hipLaunchKernelGGL(kernel, grid, dim3(KV4_MANY_WAVES * 64), 0, s, p, r, q, o, heads, scale, a.splits, a.row_blocks, part);
       };
       p16 ? go(kv4_attn_many_kernel<T, HD, true>) : go(kv4_attn_many_kernel<T, HD, false>);
       if (a.splits > 1)

@@ -1191,16 +1191,19 @@ __global__ __launch_bounds__(256, 4) void kv4_attn_one_kernel(Kv4Pool p, Kv4Rows
 
 // ---- many query rows ----
 //
-// 128 query rows of one key head, 32 a wave.  Here the products count, and the 32x32x16 form has the higher rate; codes are
-// turned into operands once for all four waves: every wave does so for 32 of a tile's 128 keys and leaves the fragments in
-// LDS, 16 bytes a lane and side by side, as the waves read them.  With lane = 32 h + c, a product's rows and columns c and its
+// 256 query rows of one key head, 32 a wave.  Here the products count, and the 32x32x16 form has the higher rate; codes are
+// turned into operands once for all eight waves, as fragments in LDS, 16 bytes a lane and side by side as the waves read them:
+// waves 0 .. 3 make 32 keys each of a tile of 128, waves 4 .. 7 their values.  LDS holds two tiles, so that one barrier a tile
+// is enough, and the makers of keys do so in front of their products, those of values behind them: a SIMD has one wave of
+// either kind, whose vector and matrix instructions then overlap.  With lane = 32 h + c, a product's rows and columns c and its
 // contraction 8 h + i, the operands follow the same ideas as above:
 //  * K: half h of key c's row, 8 elements a product, and a product of the middles (two groups a half with head_dim 128);
 //  * S^T leaves the lane with keys 8 a + 4 h + b (a, b < 4) of query c; product n of V^T P^T contracts over a = 2 n and 2 n + 1;
 //  * V: row c of block e is element (HD / 32) c + e, and the lane's outputs are HD / 8 elements in a row for every a, of group a
 //    (head_dim 64: a / 2).  Rows of the further block: 4 x the group's middle, 4 x + 1 ones, 4 x + 2 the group's NaN marks.
 // Weights enter as one binary16 number here: their rounding is as large as that of a binary16 output.
-#define KV4_MANY_ROWS 128
+#define KV4_MANY_ROWS 256
+#define KV4_MANY_WAVES 8
 
 __device__ __forceinline__ f16v kv4_mfma(h8 a, h8 b, f16v c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ float kv4_max_over_halves(float v) {
@@ -1214,26 +1217,20 @@ struct Kv4Operands {
   static constexpr int FRAGS = KS + 1 + 2 * (NE + 1);         // fragments of 32 keys
 };
 
-// 32 keys as they lie in the pool: half h of key c's row, the lane's (HD / 32) elements of 16 values
-template <int HD>
-struct Kv4Raw {
-  u32x4 k[HD / 64];
-  u32x2 kp;
-  u32 v[16], vp[16];
-};
-
 template <class T, int HD, bool P16>
-__global__ __launch_bounds__(256, 2) void kv4_attn_many_kernel(Kv4Pool p, Kv4Rows r, Kv4View q, Kv4View o, int heads, float scale,
-                                                               int splits, int row_blocks, float* part) {
+__global__ __launch_bounds__(KV4_MANY_WAVES * 64, 2) void kv4_attn_many_kernel(Kv4Pool p, Kv4Rows r, Kv4View q, Kv4View o, int heads,
+                                                                               float scale, int splits, int row_blocks, float* part) {
   using Op = Kv4Operands<HD>;
   constexpr int KS = Op::KS, NE = Op::NE;
-  __shared__ __attribute__((aligned(16))) h8 s_frag[KV4_WAVES][Op::FRAGS][64];
-  __shared__ __attribute__((aligned(16))) u32 s_rows[P16 ? 1 : KV4_WAVES][KV4_TILE];
-  __shared__ u32 s_has[KV4_WAVES];
+  __shared__ __attribute__((aligned(16))) h8 s_frag[2][KV4_WAVES][Op::FRAGS][64];
+  __shared__ __attribute__((aligned(16))) u32 s_rows[P16 ? 1 : KV4_MANY_WAVES][KV4_TILE];
+  __shared__ u32 s_has[2][KV4_WAVES];
   Kv4Work w = kv4_work(r, blockIdx.x, splits, p.kv_heads, row_blocks);
   w.rb = row_blocks - 1 - w.rb;                                            // the longest first
   const int tid = threadIdx.x, lane = tid & 63, c = lane & 31, h = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int sub = wave & 3;                                                // the wave makes the operands of this part of a tile
+  const bool makes_keys = wave < 4;
   const Kv4Seq s = kv4_seq(r, w.b);
   const int share_heads = heads / p.kv_heads, rows = min(s.rows, r.max_rows) * share_heads;
   const int f0 = w.rb * KV4_MANY_ROWS;
@@ -1278,52 +1275,61 @@ __global__ __launch_bounds__(256, 2) void kv4_attn_many_kernel(Kv4Pool p, Kv4Row
       return Kv4Listed{s_rows[wave]};
     }
   };
-  const char *kc = kv4_codes<HD>(p, 0, w.head), *kp = kv4_params<HD>(p, 0, w.head);
-  const char *vc = kv4_codes<HD>(p, 1, w.head), *vp = kv4_params<HD>(p, 1, w.head);
-  Kv4Raw<HD> raw;
+  // 32 keys as they lie in the pool: half h of key c's row; or the lane's HD / 32 elements of 16 values
+  u32x4 rk[HD / 64];
+  u32x2 rkp;
+  u32 rv[16], rvp[16];
   u32 has = 0;
   auto fetch = [&](const auto& where) {
-    const char* a = where.split(kc, HD / 2, c) + h * (HD / 4);
+    const char *codes = kv4_codes<HD>(p, makes_keys ? 0 : 1, w.head), *params = kv4_params<HD>(p, makes_keys ? 0 : 1, w.head);
+    if (makes_keys) {
+      const char* a = where.split(codes, HD / 2, c) + h * (HD / 4);
 #pragma unroll
-    for (int n = 0; n < HD / 64; ++n) raw.k[n] = *as_global(reinterpret_cast<const u32x4*>(a + 16 * n));
-    const char* b = where.split(kp, HD / 8, c) + h * (HD / 16);
-    if (HD == 128) raw.kp = *as_global(reinterpret_cast<const u32x2*>(b));
-    else raw.kp = u32x2{*as_global(reinterpret_cast<const u32*>(b)), 0};
+      for (int n = 0; n < HD / 64; ++n) rk[n] = *as_global(reinterpret_cast<const u32x4*>(a + 16 * n));
+      const char* b = where.split(params, HD / 8, c) + h * (HD / 16);
+      if (HD == 128) rkp = *as_global(reinterpret_cast<const u32x2*>(b));
+      else rkp = u32x2{*as_global(reinterpret_cast<const u32*>(b)), 0};
+    } else {
 #pragma unroll
-    for (int n = 0; n < 16; ++n) {                     // key 16 (n / 8) + 8 (n / 4 % 2) + 4 h + n % 4
-      const u32 i = 8 * (n >> 2 & 1) + 4 * h + (n & 3);
-      const char* x = where.at(vc, HD / 2, n >> 3, i) + c * (HD / 64);
-      raw.v[n] = HD == 128 ? (u32)*as_global(reinterpret_cast<const u16*>(x)) : (u32)*as_global(reinterpret_cast<const unsigned char*>(x));
-      raw.vp[n] = *as_global(reinterpret_cast<const u32*>(where.at(vp, HD / 8, n >> 3, i) + (c * (HD / 32) / KV4_GROUP) * 4));
+      for (int n = 0; n < 16; ++n) {                   // key 16 (n / 8) + 8 (n / 4 % 2) + 4 h + n % 4
+        const u32 i = 8 * (n >> 2 & 1) + 4 * h + (n & 3);
+        const char* x = where.at(codes, HD / 2, n >> 3, i) + c * (HD / 64);
+        rv[n] = HD == 128 ? (u32)*as_global(reinterpret_cast<const u16*>(x)) : (u32)*as_global(reinterpret_cast<const unsigned char*>(x));
+        rvp[n] = *as_global(reinterpret_cast<const u32*>(where.at(params, HD / 8, n >> 3, i) + (c * (HD / 32) / KV4_GROUP) * 4));
+      }
     }
   };
   const Kv4Bits bits;
   const u32 mid_row = (c & 3) == 0 ? ~0u : 0u, one_row = (c & 3) == 1 ? 0x3c003c00u : 0u;
-  // the wave's 32 keys as fragments: K's KS, their middles, then for either half of the keys V's NE and theirs
-  auto produce = [&]() {
-    h8(*out)[64] = s_frag[wave];
+  // 32 keys as fragments: K's KS, their middles, then for either half of the keys V's NE and theirs
+  auto produce = [&](int buf) {
+    h8(*out)[64] = s_frag[buf][sub];
+    if (makes_keys) {
 #pragma unroll
-    for (int n = 0; n < KS; ++n) {
-      const u32 g = HD == 128 ? raw.kp[n >> 2] : raw.kp[0];
-      const h2 step = kv4_h2(kv4_lo16(g, g));
-      h2 d[4];
-      bits.unpack(raw.k[n >> 2][n & 3], d);
-      out[n][lane] = __builtin_bit_cast(h8, u32x4{kv4_u32(d[0] * step), kv4_u32(d[1] * step), kv4_u32(d[2] * step), kv4_u32(d[3] * step)});
+      for (int n = 0; n < KS; ++n) {
+        const u32 g = HD == 128 ? rkp[n >> 2] : rkp[0];
+        const h2 step = kv4_h2(kv4_lo16(g, g));
+        h2 d[4];
+        bits.unpack(rk[n >> 2][n & 3], d);
+        out[n][lane] = __builtin_bit_cast(h8, u32x4{kv4_u32(d[0] * step), kv4_u32(d[1] * step), kv4_u32(d[2] * step), kv4_u32(d[3] * step)});
+      }
+      const half_t m0 = kv4_h2(rkp[0])[1], m1 = HD == 128 ? kv4_h2(rkp[1])[1] : (half_t)0;
+      out[KS][lane] = h8{m0, m0, m0, m1, m1, m1, 0, 0};
+      if (lane == 0) s_has[buf][sub] = has;
+      return;
     }
-    const half_t m0 = kv4_h2(raw.kp[0])[1], m1 = HD == 128 ? kv4_h2(raw.kp[1])[1] : (half_t)0;
-    out[KS][lane] = h8{m0, m0, m0, m1, m1, m1, 0, 0};
     u32 marks = 0;
-    h2 all = kv4_h2(raw.vp[0]);
+    h2 all = kv4_h2(rvp[0]);
 #pragma unroll
-    for (int n = 1; n < 16; ++n) all += kv4_h2(raw.vp[n]);
+    for (int n = 1; n < 16; ++n) all += kv4_h2(rvp[n]);
     if (~has || __any(!(all[1] == all[1]))) {
 #pragma unroll
       for (int n = 0; n < 16; ++n) {
-        const half_t mid = kv4_h2(raw.vp[n])[1];
+        const half_t mid = kv4_h2(rvp[n])[1];
         const int key = 16 * (n >> 3) + 8 * (n >> 2 & 1) + 4 * h + (n & 3);
         const bool gone = !(has >> key & 1), nan = !(mid == mid);
         if (nan && !gone) marks |= 1u << n;
-        if (gone || nan) raw.vp[n] = 0;
+        if (gone || nan) rvp[n] = 0;
       }
     }
 #pragma unroll
@@ -1332,12 +1338,12 @@ __global__ __launch_bounds__(256, 2) void kv4_attn_many_kernel(Kv4Pool p, Kv4Row
 #pragma unroll
       for (int a = 0; a < 4; ++a) {
         const int n = 8 * t + 2 * a;
-        const h2 step = kv4_h2(kv4_lo16(raw.vp[n], raw.vp[n + 1]));
+        const h2 step = kv4_h2(kv4_lo16(rvp[n], rvp[n + 1]));
         h2 d[4];
-        bits.unpack(raw.v[n] | raw.v[n + 1] << 16, d);
+        bits.unpack(rv[n] | rv[n + 1] << 16, d);
 #pragma unroll
         for (int i = 0; i < NE; ++i) w4[i][a] = kv4_u32(d[i] * step);
-        mids[a] = (kv4_hi16(raw.vp[n], raw.vp[n + 1]) & mid_row) | one_row;
+        mids[a] = (kv4_hi16(rvp[n], rvp[n + 1]) & mid_row) | one_row;
       }
       if (__any(marks)) {
 #pragma unroll
@@ -1351,14 +1357,13 @@ __global__ __launch_bounds__(256, 2) void kv4_attn_many_kernel(Kv4Pool p, Kv4Row
       for (int i = 0; i < NE; ++i) out[KS + 1 + t * (NE + 1) + i][lane] = __builtin_bit_cast(h8, w4[i]);
       out[KS + 1 + t * (NE + 1) + NE][lane] = __builtin_bit_cast(h8, mids);
     }
-    if (lane == 0) s_has[wave] = has;
   };
 
   u32x2 at{0, 0};
   if (t0 < t1) {
-    const u32x2 at0 = look(t0 + wave);
-    at = look(t0 + KV4_WAVES + wave);
-    fetch(place(t0 + wave, at0, has));
+    const u32x2 at0 = look(t0 + sub);
+    at = look(t0 + KV4_WAVES + sub);
+    fetch(place(t0 + sub, at0, has));
   }
   // queries, in K's order and scaled as above
   h8 qf[KS], sums;
@@ -1405,20 +1410,26 @@ __global__ __launch_bounds__(256, 2) void kv4_attn_many_kernel(Kv4Pool p, Kv4Row
 #pragma unroll
     for (int i = 0; i < 16; ++i) acc[e][i] = 0.f;
   float m = -INFINITY;
-  for (int t = t0; t < t1; t += KV4_WAVES) {
-    produce();
+  // the next tile's operands into the other buffer, and the request for the one behind it
+  auto prepare = [&](int t, int buf) {
+    produce(buf);
     if (t + KV4_WAVES < t1) {
       const u32x2 now = at;
-      at = look(t + 2 * KV4_WAVES + wave);
-      fetch(place(t + KV4_WAVES + wave, now, has));
+      at = look(t + 2 * KV4_WAVES + sub);
+      fetch(place(t + KV4_WAVES + sub, now, has));
     }
+  };
+  if (t0 < t1) prepare(t0, 0);
+  kv4_barrier();
+  for (int t = t0, buf = 0; t < t1; t += KV4_WAVES, buf ^= 1) {
+    const bool more = t + KV4_WAVES < t1;
+    if (makes_keys && more) prepare(t + KV4_WAVES, buf ^ 1);
     __builtin_amdgcn_sched_barrier(0);
-    kv4_barrier();
     for (int n = 0; n < KV4_WAVES; ++n) {
       const int u0 = (t + n) * KV4_TILE;
       if (u0 > last_limit || u0 >= n_keys) break;
-      const u32 there_mask = __builtin_amdgcn_readfirstlane(s_has[n]);
-      const h8(*in)[64] = s_frag[n];
+      const u32 there_mask = __builtin_amdgcn_readfirstlane(s_has[buf][n]);
+      const h8(*in)[64] = s_frag[buf][n];
       f16v sc;
 #pragma unroll
       for (int i = 0; i < 16; ++i) sc[i] = 0.f;
@@ -1455,6 +1466,8 @@ __global__ __launch_bounds__(256, 2) void kv4_attn_many_kernel(Kv4Pool p, Kv4Row
         for (int e = 0; e <= NE; ++e) acc[e] = kv4_mfma(in[KS + 1 + k * (NE + 1) + e][lane], pr, acc[e]);
       }
     }
+    __builtin_amdgcn_sched_barrier(0);
+    if (!makes_keys && more) prepare(t + KV4_WAVES, buf ^ 1);
     kv4_barrier();
   }
 
