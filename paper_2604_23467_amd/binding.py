@@ -283,17 +283,16 @@ class KV4Rows:
 
     def __init__(self, lens, page_table, max_rows=1, row_start=None, max_len=0):
         import torch
-        index = lens.get_device()
+        index, shape, int32 = lens.get_device(), page_table.shape, torch.int32
         for t in (lens, page_table) if row_start is None else (lens, page_table, row_start):
-            if t.dtype != torch.int32 or not t.is_contiguous() or not t.is_cuda or t.get_device() != index:
+            if t.dtype is not int32 or not t.is_contiguous() or not t.is_cuda or t.get_device() != index:
                 raise ValueError("lens, page_table and row_start must be contiguous int32 tensors of one CUDA device")
         n = lens.shape[0]
-        if lens.dim() != 1 or page_table.dim() != 2 or page_table.shape[0] != n or \
-                (row_start is not None and row_start.shape != (n + 1,)):
+        if lens.dim() != 1 or len(shape) != 2 or shape[0] != n or (row_start is not None and row_start.shape != (n + 1,)):
             raise ValueError("lens [n_seqs], page_table [n_seqs, pages] and row_start [n_seqs + 1] do not fit together")
         self.lens, self.page_table, self.row_start, self.index = lens, page_table, row_start, index
         self.c = LLKV4Rows(None if row_start is None else row_start.data_ptr(), lens.data_ptr(), page_table.data_ptr(),
-                           n, max_rows, 0, page_table.shape[1], max_len)
+                           n, max_rows, 0, shape[1], max_len)
 
 
 def _kv4_view(t, name, cache, heads, n_rows, dtype):
@@ -305,36 +304,34 @@ def _kv4_view(t, name, cache, heads, n_rows, dtype):
     return LLKV4View(t.data_ptr(), strides[0], strides[1])
 
 
-def _kv4_type(dtype):
-    import torch
-    if dtype is torch.float16:
-        return LL_F16
-    if dtype is torch.bfloat16:
-        return LL_BF16
-    raise ValueError("rows are float16 or bfloat16, not %s" % dtype)
-
-
-def _kv4_do(cache, rows, n_rows, stream, call):
-    """call(stream handle) with the pool's device as the current one, and, where ``stream`` is given instead of torch's current
-    one, with it as the current stream, so that what the call allocates belongs to it."""
-    import torch
+def _kv4_enter(torch, cache, rows, n_rows, dtype, stream):
+    """Checks of every call: the row type's code, the handle of the stream to work on, and what has to be entered for the call so
+    that the pool's device and a given ``stream`` are torch's current ones (and own what the call allocates): None mostly."""
     if rows.index != cache.index:
         raise ValueError("lens and page_table must be on the pool's device")
+    if dtype is not torch.float16 and dtype is not torch.bfloat16:
+        raise ValueError("rows are float16 or bfloat16, not %s" % dtype)
     rows.c.n_rows = n_rows
+    kind = LL_F16 if dtype is torch.float16 else LL_BF16
     if stream is not None:
-        with torch.cuda.stream(stream):
-            return call(stream.cuda_stream)
-    if torch._C._cuda_getDevice() != cache.index:
-        with torch.cuda.device(cache.index):
-            return call(torch._C._cuda_getCurrentRawStream(cache.index))
-    return call(torch._C._cuda_getCurrentRawStream(cache.index))
+        if stream.device.index != cache.index:
+            raise ValueError("the stream must be one of the pool's device")
+        return kind, stream.cuda_stream, torch.cuda.stream(stream)
+    on = None if torch._C._cuda_getDevice() == cache.index else torch.cuda.device(cache.index)
+    return kind, torch._C._cuda_getCurrentRawStream(cache.index), on
 
 
 def ll_kv4_write(cache, rows, k, v, stream=None):
     """Quantises rows of k and v, [rows, n_kv_heads, head_dim] float16 or bfloat16, into the cache."""
-    n, dtype = k.shape[0], k.dtype
-    kind, kv, vv = _kv4_type(dtype), _kv4_view(k, "k", cache, cache.n_kv_heads, n, dtype), _kv4_view(v, "v", cache, cache.n_kv_heads, n, dtype)
-    _kv4_do(cache, rows, n, stream, lambda s: _check(load().ll_kv4_write(C.byref(cache.c), C.byref(rows.c), kind, C.byref(kv), C.byref(vv), s)))
+    import torch
+    n, dtype, heads = k.shape[0], k.dtype, cache.n_kv_heads
+    kind, s, on = _kv4_enter(torch, cache, rows, n, dtype, stream)
+    if on is not None:
+        with on:
+            return ll_kv4_write(cache, rows, k, v)
+    rc = load().ll_kv4_write(cache.c, rows.c, kind, _kv4_view(k, "k", cache, heads, n, dtype), _kv4_view(v, "v", cache, heads, n, dtype), s)
+    if rc < 0:
+        _check(rc)
 
 
 def ll_kv4_read(cache, rows, k=None, v=None, n_rows=0, dtype=None, stream=None):
@@ -342,20 +339,25 @@ def ll_kv4_read(cache, rows, k=None, v=None, n_rows=0, dtype=None, stream=None):
     import torch
     if k is not None:
         n_rows, dtype = k.shape[0], k.dtype
-    kind = _kv4_type(dtype)
-
-    def call(s):
-        a, b = (k, v) if k is not None else torch.empty((2, n_rows, cache.n_kv_heads, cache.head_dim), dtype=dtype, device=cache.device)
-        kv, vv = _kv4_view(a, "k", cache, cache.n_kv_heads, n_rows, dtype), _kv4_view(b, "v", cache, cache.n_kv_heads, n_rows, dtype)
-        _check(load().ll_kv4_read(C.byref(cache.c), C.byref(rows.c), kind, C.byref(kv), C.byref(vv), s))
-        return a, b
-    return _kv4_do(cache, rows, n_rows, stream, call)
+    kind, s, on = _kv4_enter(torch, cache, rows, n_rows, dtype, stream)
+    if on is not None:
+        with on:
+            return ll_kv4_read(cache, rows, k, v, n_rows, dtype)
+    heads = cache.n_kv_heads
+    if k is None:
+        k = torch.empty((n_rows, heads, cache.head_dim), dtype=dtype, device=cache.device)
+        v = torch.empty((n_rows, heads, cache.head_dim), dtype=dtype, device=cache.device)
+    rc = load().ll_kv4_read(cache.c, rows.c, kind, _kv4_view(k, "k", cache, heads, n_rows, dtype),
+                            _kv4_view(v, "v", cache, heads, n_rows, dtype), s)
+    if rc < 0:
+        _check(rc)
+    return k, v
 
 
 def ll_kv4_attention_workspace_bytes(cache, rows, n_heads, n_rows):
     """Bytes of workspace of such an attention call (host arithmetic)."""
     rows.c.n_rows = n_rows
-    return int(load().ll_kv4_attention_workspace_bytes(C.byref(cache.c), C.byref(rows.c), n_heads))
+    return load().ll_kv4_attention_workspace_bytes(cache.c, rows.c, n_heads)
 
 
 def ll_kv4_attention(cache, rows, q, k=None, v=None, scale=0.0, out=None, workspace=None, stream=None):
@@ -366,26 +368,29 @@ def ll_kv4_attention(cache, rows, q, k=None, v=None, scale=0.0, out=None, worksp
     if len(shape) != 3:
         raise ValueError("q must be [rows, heads, %d]" % cache.head_dim)
     n, heads = shape[0], shape[1]
-    kind, qv = _kv4_type(dtype), _kv4_view(q, "q", cache, heads, n, dtype)
-    kv = None if k is None else C.byref(_kv4_view(k, "k", cache, cache.n_kv_heads, n, dtype))
-    vv = None if v is None else C.byref(_kv4_view(v, "v", cache, cache.n_kv_heads, n, dtype))
-
-    def call(s):
-        o = torch.empty(shape, dtype=dtype, device=cache.device) if out is None else out
-        ov = _kv4_view(o, "out", cache, heads, n, dtype)
-        w, nbytes = workspace, 0
-        if w is None:
-            nbytes = ll_kv4_attention_workspace_bytes(cache, rows, heads, n)
-            if nbytes:
-                w = torch.empty(nbytes, dtype=torch.uint8, device=cache.device)
-        else:
-            if w.get_device() != cache.index or not w.is_contiguous():
-                raise ValueError("workspace must be a contiguous tensor on the pool's device")
-            nbytes = w.numel() * w.element_size()
-        _check(load().ll_kv4_attention(C.byref(cache.c), C.byref(rows.c), kind, heads, scale, C.byref(qv), kv, vv, C.byref(ov),
-                                       w.data_ptr() if nbytes else None, nbytes, s))
-        return o
-    return _kv4_do(cache, rows, n, stream, call)
+    kind, s, on = _kv4_enter(torch, cache, rows, n, dtype, stream)
+    if on is not None:
+        with on:
+            return ll_kv4_attention(cache, rows, q, k, v, scale, out, workspace)
+    qv = _kv4_view(q, "q", cache, heads, n, dtype)
+    kv = None if k is None else _kv4_view(k, "k", cache, cache.n_kv_heads, n, dtype)
+    vv = None if v is None else _kv4_view(v, "v", cache, cache.n_kv_heads, n, dtype)
+    if out is None:
+        out = torch.empty(shape, dtype=dtype, device=cache.device)
+    ov = _kv4_view(out, "out", cache, heads, n, dtype)
+    lib = load()
+    if workspace is None:
+        nbytes = lib.ll_kv4_attention_workspace_bytes(cache.c, rows.c, heads)
+        if nbytes:
+            workspace = torch.empty(nbytes, dtype=torch.uint8, device=cache.device)
+    elif workspace.get_device() != cache.index or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous tensor on the pool's device")
+    else:
+        nbytes = workspace.numel() * workspace.element_size()
+    rc = lib.ll_kv4_attention(cache.c, rows.c, kind, heads, scale, qv, kv, vv, ov, workspace.data_ptr() if nbytes else None, nbytes, s)
+    if rc < 0:
+        _check(rc)
+    return out
 
 
 class Session:

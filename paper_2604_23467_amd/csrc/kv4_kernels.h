@@ -1276,26 +1276,28 @@ __global__ __launch_bounds__(KV4_MANY_WAVES * 64, 2) void kv4_attn_many_kernel(K
     }
   };
   // 32 keys as they lie in the pool: half h of key c's row; or the lane's HD / 32 elements of 16 values
-  u32x4 rk[HD / 64];
-  u32x2 rkp;
-  u32 rv[16], rvp[16];
+  u32 raw[32];               // K: codes, then 2 parameters; V: codes, then parameters (the same registers for either)
   u32 has = 0;
   auto fetch = [&](const auto& where) {
     const char *codes = kv4_codes<HD>(p, makes_keys ? 0 : 1, w.head), *params = kv4_params<HD>(p, makes_keys ? 0 : 1, w.head);
     if (makes_keys) {
       const char* a = where.split(codes, HD / 2, c) + h * (HD / 4);
 #pragma unroll
-      for (int n = 0; n < HD / 64; ++n) rk[n] = *as_global(reinterpret_cast<const u32x4*>(a + 16 * n));
+      for (int n = 0; n < HD / 64; ++n) {
+        const u32x4 x = *as_global(reinterpret_cast<const u32x4*>(a + 16 * n));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) raw[4 * n + i] = x[i];
+      }
       const char* b = where.split(params, HD / 8, c) + h * (HD / 16);
-      if (HD == 128) rkp = *as_global(reinterpret_cast<const u32x2*>(b));
-      else rkp = u32x2{*as_global(reinterpret_cast<const u32*>(b)), 0};
+      raw[8] = *as_global(reinterpret_cast<const u32*>(b));
+      if (HD == 128) raw[9] = *as_global(reinterpret_cast<const u32*>(b + 4));
     } else {
 #pragma unroll
       for (int n = 0; n < 16; ++n) {                   // key 16 (n / 8) + 8 (n / 4 % 2) + 4 h + n % 4
         const u32 i = 8 * (n >> 2 & 1) + 4 * h + (n & 3);
         const char* x = where.at(codes, HD / 2, n >> 3, i) + c * (HD / 64);
-        rv[n] = HD == 128 ? (u32)*as_global(reinterpret_cast<const u16*>(x)) : (u32)*as_global(reinterpret_cast<const unsigned char*>(x));
-        rvp[n] = *as_global(reinterpret_cast<const u32*>(where.at(params, HD / 8, n >> 3, i) + (c * (HD / 32) / KV4_GROUP) * 4));
+        raw[n] = HD == 128 ? (u32)*as_global(reinterpret_cast<const u16*>(x)) : (u32)*as_global(reinterpret_cast<const unsigned char*>(x));
+        raw[16 + n] = *as_global(reinterpret_cast<const u32*>(where.at(params, HD / 8, n >> 3, i) + (c * (HD / 32) / KV4_GROUP) * 4));
       }
     }
   };
@@ -1307,29 +1309,29 @@ __global__ __launch_bounds__(KV4_MANY_WAVES * 64, 2) void kv4_attn_many_kernel(K
     if (makes_keys) {
 #pragma unroll
       for (int n = 0; n < KS; ++n) {
-        const u32 g = HD == 128 ? rkp[n >> 2] : rkp[0];
+        const u32 g = raw[8 + (HD == 128 ? n >> 2 : 0)];
         const h2 step = kv4_h2(kv4_lo16(g, g));
         h2 d[4];
-        bits.unpack(rk[n >> 2][n & 3], d);
+        bits.unpack(raw[n], d);
         out[n][lane] = __builtin_bit_cast(h8, u32x4{kv4_u32(d[0] * step), kv4_u32(d[1] * step), kv4_u32(d[2] * step), kv4_u32(d[3] * step)});
       }
-      const half_t m0 = kv4_h2(rkp[0])[1], m1 = HD == 128 ? kv4_h2(rkp[1])[1] : (half_t)0;
+      const half_t m0 = kv4_h2(raw[8])[1], m1 = HD == 128 ? kv4_h2(raw[9])[1] : (half_t)0;
       out[KS][lane] = h8{m0, m0, m0, m1, m1, m1, 0, 0};
       if (lane == 0) s_has[buf][sub] = has;
       return;
     }
     u32 marks = 0;
-    h2 all = kv4_h2(rvp[0]);
+    h2 all = kv4_h2(raw[16]);
 #pragma unroll
-    for (int n = 1; n < 16; ++n) all += kv4_h2(rvp[n]);
+    for (int n = 1; n < 16; ++n) all += kv4_h2(raw[16 + n]);
     if (~has || __any(!(all[1] == all[1]))) {
 #pragma unroll
       for (int n = 0; n < 16; ++n) {
-        const half_t mid = kv4_h2(rvp[n])[1];
+        const half_t mid = kv4_h2(raw[16 + n])[1];
         const int key = 16 * (n >> 3) + 8 * (n >> 2 & 1) + 4 * h + (n & 3);
         const bool gone = !(has >> key & 1), nan = !(mid == mid);
         if (nan && !gone) marks |= 1u << n;
-        if (gone || nan) rvp[n] = 0;
+        if (gone || nan) raw[16 + n] = 0;
       }
     }
 #pragma unroll
@@ -1338,12 +1340,12 @@ __global__ __launch_bounds__(KV4_MANY_WAVES * 64, 2) void kv4_attn_many_kernel(K
 #pragma unroll
       for (int a = 0; a < 4; ++a) {
         const int n = 8 * t + 2 * a;
-        const h2 step = kv4_h2(kv4_lo16(rvp[n], rvp[n + 1]));
+        const h2 step = kv4_h2(kv4_lo16(raw[16 + n], raw[17 + n]));
         h2 d[4];
-        bits.unpack(rv[n] | rv[n + 1] << 16, d);
+        bits.unpack(raw[n] | raw[n + 1] << 16, d);
 #pragma unroll
         for (int i = 0; i < NE; ++i) w4[i][a] = kv4_u32(d[i] * step);
-        mids[a] = (kv4_hi16(rvp[n], rvp[n + 1]) & mid_row) | one_row;
+        mids[a] = (kv4_hi16(raw[16 + n], raw[17 + n]) & mid_row) | one_row;
       }
       if (__any(marks)) {
 #pragma unroll
