@@ -299,8 +299,7 @@ int ll_batch_dbg_time_steps(int32_t k, float *ms_out);
  * The three calls below work on one layer's pool, with or without an initialised instance, on the stream that they are given
  * (a hipStream_t; NULL: the default stream) of the current device, which the memory has to belong to.  They return when their
  * kernels are queued, hold no state between calls, allocate nothing, and can be captured into a graph.  Every pointer is a
- * DEVICE pointer and stays the caller's.  ll_batch_open_kv runs batched
- * decoding on such pools.
+ * DEVICE pointer and stays the caller's.  ll_batch_open_kv runs batched decoding on such pools.
  * Errors as above: LL_E_BAD_ARG, LL_E_BAD_CONFIG (a shape that is not supported), LL_E_WORKSPACE (pool or workspace too small
  * or misaligned), LL_E_HIP; but for LL_E_HIP nothing was queued. */
 enum { LL_F16 = 0, LL_BF16 = 1 }; /* type of the rows at the calls' borders: binary16, bfloat16 */
@@ -351,6 +350,7 @@ size_t ll_kv4_attention_workspace_bytes(const ll_kv4_cache *cache, const ll_kv4_
  * them; n_heads / n_kv_heads query heads in a row share a key head.  Scores are multiplied by scale (0: 1 / sqrt(head_dim)).
  * k and v (both NULL, or both given) are the same rows' keys and values: they are written to the cache first, as by
  * ll_kv4_write, and attended as they are held.  Rows that see no position give zeros.  out must not overlap q, k or v.
+ * LL_E_BAD_ARG for a page table of more than 2^30 positions and for more than 2^30 query rows a key head.
  * workspace (256-byte aligned) holds nothing between calls; calls that may run at the same time need one each. */
 int ll_kv4_attention(const ll_kv4_cache *cache, const ll_kv4_rows *rows, int32_t dtype, int32_t n_heads, float scale,
                      const ll_kv4_view *q, const ll_kv4_view *k, const ll_kv4_view *v, const ll_kv4_view *out, void *workspace,

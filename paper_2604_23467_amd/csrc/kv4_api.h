@@ -65,14 +65,20 @@ int ll_kv4_attention(const ll_kv4_cache* cache, const ll_kv4_rows* rows, int32_t
     return fail(LL_E_BAD_CONFIG, "%s: n_heads = %d, need a multiple of n_kv_heads = %d up to %d", who, n_heads, p.kv_heads, kKv4MaxHeads);
   if (!(scale >= 0.f) || !(scale < INFINITY)) return fail(LL_E_BAD_ARG, "%s: scale = %g, need a finite value >= 0", who, (double)scale);
   if (!k != !v) return fail(LL_E_BAD_ARG, "%s: k and v come together", who);
+  if ((int64_t)r.table_stride * p.page_tokens > kKv4MaxPositions)
+    return fail(LL_E_BAD_ARG, "%s: a page table of %d pages of %d positions, at most %d positions", who, r.table_stride, p.page_tokens,
+                kKv4MaxPositions);
+  if ((int64_t)r.max_rows * (n_heads / p.kv_heads) > kKv4MaxPositions)
+    return fail(LL_E_BAD_ARG, "%s: %d rows of %d heads a key head, at most %d", who, r.max_rows, n_heads / p.kv_heads, kKv4MaxPositions);
   if (r.n_seqs == 0 || r.n_rows == 0) return LL_OK;
   if ((rc = kv4_check_view(who, "q", q, rows, n_heads, cache->head_dim, false, &qq)) != LL_OK ||
       (rc = kv4_check_view(who, "out", out, rows, n_heads, cache->head_dim, true, &oo)) != LL_OK) return rc;
   if (k && ((rc = kv4_check_view(who, "k", k, rows, p.kv_heads, cache->head_dim, false, &kk)) != LL_OK ||
             (rc = kv4_check_view(who, "v", v, rows, p.kv_heads, cache->head_dim, false, &vv)) != LL_OK)) return rc;
   const Kv4Plan a = kv4_plan(p, r, rows->max_len, cache->head_dim, n_heads);
-  if (a.works * a.splits >= 1 << 24)
-    return fail(LL_E_BAD_ARG, "%s: %lld workgroups, a launch holds %d", who, (long long)(a.works * a.splits), (1 << 24) - 1);
+  const int most = a.many ? 1 << 23 : 1 << 24;      // of 512 or 256 threads, which stay inside 32 bits
+  if (a.works * a.splits >= most)
+    return fail(LL_E_BAD_ARG, "%s: %lld workgroups, a launch holds %d", who, (long long)(a.works * a.splits), most - 1);
   if (workspace_bytes < a.bytes || (a.bytes && !workspace))
     return fail(LL_E_WORKSPACE, "%s: workspace has %zu bytes, %zu needed", who, workspace_bytes, a.bytes);
   if (a.bytes && reinterpret_cast<uintptr_t>(workspace) % kAlign)

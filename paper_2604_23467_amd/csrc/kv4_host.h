@@ -6,6 +6,8 @@ namespace {
 
 constexpr int kKv4MaxRows = 1 << 26;     // pool rows: a row's byte offset within a head's codes stays inside 32 bits
 constexpr int kKv4MaxHeads = 4096;
+constexpr int kKv4MaxPositions = 1 << 30;      // of a page table that attention reads; query rows of a key head: positions and rows a
+                                               // few tiles further on stay inside 32 bits
 
 int kv4_check_cache(const char* who, const ll_kv4_cache* c, bool with_pool, Kv4Pool* out) {
   if (!c) return fail(LL_E_BAD_ARG, "%s: null cache", who);
@@ -42,6 +44,8 @@ int kv4_check_rows(const char* who, const ll_kv4_rows* r, bool with_pointers, Kv
     return fail(LL_E_BAD_ARG, "%s: without row_start n_rows = %d must be n_seqs * max_rows = %d * %d", who, r->n_rows, r->n_seqs, r->max_rows);
   if (r->n_seqs >= 1 << 24 || r->n_rows >= 1 << 24)      // threads of a launch along one dimension stay inside 32 bits
     return fail(LL_E_BAD_ARG, "%s: n_seqs = %d, n_rows = %d, at most %d", who, r->n_seqs, r->n_rows, (1 << 24) - 1);
+  if ((reinterpret_cast<uintptr_t>(r->row_start) | reinterpret_cast<uintptr_t>(r->len) | reinterpret_cast<uintptr_t>(r->page_table)) % 4)
+    return fail(LL_E_BAD_ARG, "%s: row_start, len or page_table is not aligned to its elements", who);
   if (with_pointers && r->n_seqs > 0 && (!r->len || !r->page_table)) return fail(LL_E_BAD_ARG, "%s: null len or page_table", who);
   if (out) {
     *out = Kv4Rows{};

@@ -394,6 +394,11 @@ __device__ __forceinline__ Kv4Work kv4_work(const Kv4Rows& r, int id, int splits
   w.b = r.order ? kv4_scalar(r.order + id / row_blocks) : id / row_blocks;
   return w;
 }
+// Positions that the sequence's row j sees: none behind what the page table has entries for (at most 2^30, the host's check),
+// however large the length that lies in memory
+__device__ __forceinline__ int kv4_keys(const Kv4Pool& p, const Kv4Rows& r, const Kv4Seq& s, int j) {
+  return max(min(s.len - s.rows + j + 1, r.table_stride * p.page_tokens), 0);
+}
 // Tiles of a share when `tiles` of them are dealt to `splits` workgroups: whole rounds of the waves
 __device__ __forceinline__ int kv4_share(int tiles, int splits) {
   return ((tiles + splits - 1) / splits + KV4_WAVES - 1) / KV4_WAVES * KV4_WAVES;
@@ -647,7 +652,7 @@ __global__ __launch_bounds__(256, 3) void kv4_attn_few_kernel(Kv4Pool p, Kv4Rows
   const int f0 = w.rb * KV4_FEW_ROWS;
   if (f0 >= rows) return;
   const int first_limit = s.len - s.rows + f0 / share_heads;               // last position that the first query sees
-  const int n_keys = max(s.len - s.rows + min(f0 + KV4_FEW_ROWS - 1, rows - 1) / share_heads + 1, 0);
+  const int n_keys = kv4_keys(p, r, s, min(f0 + KV4_FEW_ROWS - 1, rows - 1) / share_heads);
   const int tiles = (n_keys + KV4_TILE - 1) / KV4_TILE, share = kv4_share(tiles, splits);
   const int t0 = w.split * share, t1 = min(t0 + share, tiles);
   if (w.split > 0 && t0 >= tiles) return;
@@ -931,7 +936,7 @@ __global__ __launch_bounds__(256, 4) void kv4_attn_one_kernel(Kv4Pool p, Kv4Rows
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const Kv4Seq s = kv4_seq(r, w.b);
   if (s.rows < 1) return;
-  const int n_keys = max(s.len - s.rows + 1, 0);
+  const int n_keys = kv4_keys(p, r, s, 0);
   const int tiles = (n_keys + KV4_TILE - 1) / KV4_TILE, share = kv4_share(tiles, splits);
   const int t0 = w.split * share, end = min((t0 + share) * KV4_TILE, n_keys);
   if (w.split > 0 && t0 >= tiles) return;
@@ -1235,7 +1240,7 @@ __global__ __launch_bounds__(KV4_MANY_WAVES * 64, 2) void kv4_attn_many_kernel(K
   const int share_heads = heads / p.kv_heads, rows = min(s.rows, r.max_rows) * share_heads;
   const int f0 = w.rb * KV4_MANY_ROWS;
   if (f0 >= rows) return;
-  const int n_keys = max(s.len - s.rows + min(f0 + KV4_MANY_ROWS - 1, rows - 1) / share_heads + 1, 0);
+  const int n_keys = kv4_keys(p, r, s, min(f0 + KV4_MANY_ROWS - 1, rows - 1) / share_heads);
   const int tiles = (n_keys + KV4_TILE - 1) / KV4_TILE, share = kv4_share(tiles, splits);
   const int t0 = w.split * share, t1 = min(t0 + share, tiles);
   if (w.split > 0 && t0 >= tiles) return;
@@ -1520,7 +1525,7 @@ __global__ __launch_bounds__(256) void kv4_join_kernel(Kv4Pool p, Kv4Rows r, Kv4
   const int lane = threadIdx.x & 63, row = blockIdx.y * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int f0 = w.rb * ROWS, f = f0 + row;
   if (f >= rows) return;
-  const int n_keys = max(s.len - s.rows + min(f0 + ROWS - 1, rows - 1) / share_heads + 1, 0);
+  const int n_keys = kv4_keys(p, r, s, min(f0 + ROWS - 1, rows - 1) / share_heads);
   const int tiles = (n_keys + KV4_TILE - 1) / KV4_TILE, share = kv4_share(tiles, splits);
   const int n = tiles ? (tiles + share - 1) / share : 1;
   const float* from = part + (size_t)blockIdx.x * splits * PART;

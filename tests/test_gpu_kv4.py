@@ -252,6 +252,28 @@ def test_pages_that_are_not_there(ll):
     assert (out[60:80] == 0).all() and (out[80:95] == 0).all()
 
 
+@pytest.mark.parametrize("heads,kv_heads,rows,page", [(2, 2, 1, 16), (2, 2, 1, 7), (8, 1, 2, 16), (8, 2, 3, 7), (32, 32, 65, 16), (32, 32, 65, 7)])
+@pytest.mark.parametrize("length", [2 ** 31 - 1, 2 ** 30 + 5, 1100])
+def test_lengths_beyond_the_page_table(ll, heads, kv_heads, rows, page, length):
+    """All that the table has is seen, by every row, and the rows' own keys have no place."""
+    n, seqs = 1024 // page * page, 4 if rows > 64 else 1
+    table, pages, at = ku.paged([n] * seqs, page, seed=3, extra=0)
+    raw, pool = ku.random_pool(kv_heads, 64, pages * page, at, seed=4)
+    g = torch.Generator().manual_seed(5)
+    q = torch.randn(seqs * rows, heads, 64, generator=g).half()
+    knew = torch.randn(seqs * rows, kv_heads, 64, generator=g).half()
+    mem = dev(raw)
+    cache = ll.KV4Cache(mem, kv_heads, 64, page, pages)
+    layout = ll.KV4Rows(ints([length] * seqs), ints(table), max_rows=rows)
+    got = [ll.ll_kv4_attention(cache, layout, dev(q), **new) for new in ({}, dict(k=dev(knew), v=dev(knew)))]
+    for b in range(seqs):
+        its = slice(b * rows, (b + 1) * rows)
+        want, tol = ku.attention(q[its].double(), pool.get(0, at[b]), pool.get(1, at[b]), [n] * rows, 64 ** -0.5)
+        for out in got:
+            ku.check_attention(out[its], want, tol, "sequence %d" % b)
+    assert torch.equal(mem.cpu(), raw)
+
+
 def test_scales_and_large_scores(ll):
     attend(ll, "f16", 2, 2, 64, 16, [1, 1], [50, 700], ragged=False, scale=0.5)
     attend(ll, "bf16", 2, 1, 128, 16, [40, 3], [50, 700], scale=0.01)

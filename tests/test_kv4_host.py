@@ -84,6 +84,22 @@ def test_other_refusals():
     assert lib.ll_kv4_write(c, r, 0, v, v, None) == b.LL_E_BAD_ARG
 
 
+def test_sizes_that_would_leave_32_bits_are_refused():
+    cache, rows, view = good()
+    c, r, v = C.byref(cache), C.byref(rows), C.byref(view)
+    lib = b.load()
+    rows.table_stride = (1 << 26) + 1                            # of 16 positions
+    assert lib.ll_kv4_attention(c, r, 0, 4, 0.0, v, None, None, v, None, 0, None) == b.LL_E_BAD_ARG and "page table" in b.ll_last_error()
+    rows.table_stride, cache.n_kv_heads = 8, 1
+    rows.n_seqs, rows.n_rows, rows.max_rows = 1, 1 << 20, 1 << 20
+    assert lib.ll_kv4_attention(c, r, 0, 2048, 0.0, v, None, None, v, None, 0, None) == b.LL_E_BAD_ARG and "rows" in b.ll_last_error()
+    for field in ("len", "page_table", "row_start"):
+        cache, rows, view = good()
+        setattr(rows, field, 0x5002)
+        assert lib.ll_kv4_write(C.byref(cache), C.byref(rows), 0, C.byref(view), C.byref(view), None) == b.LL_E_BAD_ARG
+        assert "aligned" in b.ll_last_error()
+
+
 def test_nothing_to_do_is_no_error():
     cache, rows, _ = good()
     rows.n_seqs = rows.n_rows = 0
