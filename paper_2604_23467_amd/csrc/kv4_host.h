@@ -73,7 +73,6 @@ int kv4_check_view(const char* who, const char* name, const ll_kv4_view* v, cons
   out->data = v->data;
   out->row_stride = v->row_stride;
   out->head_stride = v->head_stride;
-  out->wide = reinterpret_cast<uintptr_t>(v->data) % 16 == 0 && v->row_stride % 8 == 0 && v->head_stride % 8 == 0;
   return LL_OK;
 }
 
@@ -89,7 +88,9 @@ void kv4_dispatch(int32_t dtype, int head_dim, F&& go) {
   else head_dim == 128 ? go(Kv4Bf16{}, Kv4Dim<128>{}) : go(Kv4Bf16{}, Kv4Dim<64>{});
 }
 
-// Blocks of 8 rows where that leaves every CU with work of several workgroups; single rows, whose chain is shorter, else
+// Blocks of 8 rows where they still give every CU two workgroups: reading 32 x 1 .. 1000 rows of 32 heads takes 83 us, row by
+// row 134; writing 4 x 1 .. 8190 rows of 8 heads and reading them 64, row by row 67.  Single rows, whose chain is shorter, else:
+// writing 16 rows 7.6 us, in blocks 15.3; 500 rows of 32 heads and reading them 13.8, 18.4.
 constexpr int kKv4RowBlock = 8;
 template <class F>
 void kv4_row_blocks(const Kv4Pool& p, const Kv4Rows& r, int head_dim, int layers, F&& go) {
@@ -118,7 +119,7 @@ void kv4_launch_read(hipStream_t s, int32_t dtype, int head_dim, const Kv4Pool& 
 
 // How attention is cut into workgroups: blocks of query rows, and shares of the keys where that leaves CUs idle
 struct Kv4Plan {
-  bool many;                   // row blocks of 128, else of 16
+  bool many;                   // row blocks of KV4_MANY_ROWS, else of KV4_FEW_ROWS
   int row_blocks, splits;
   int64_t works;               // (row block, key head, sequence)
   size_t bytes;                // of workspace
@@ -130,13 +131,16 @@ Kv4Plan kv4_plan(const Kv4Pool& p, const Kv4Rows& r, int max_len, int head_dim, 
   const int64_t len = max_len > 0 ? std::min<int64_t>(max_len, most) : most;
   const int64_t rounds = (len + KV4_TILE * KV4_WAVES - 1) / (KV4_TILE * KV4_WAVES);      // of the four waves over the keys
   const int64_t shares = std::max<int64_t>(1, std::min<int64_t>(rounds / 4, 64));        // at most (64: a wave's lanes, see the join)
-  // Blocks of 128 rows where they, times the shares, leave no CU idle.  One sequence of 500 rows and 32 heads, 128 such
-  // workgroups: 28.6 us, in blocks of 16 rows 21.2; six of up to 700 behind up to 2000, 1056 workgroups: 120, 160.
+  // Blocks of 256 rows where they, times the shares, leave no CU idle: there a workgroup turns codes into operands once for 16
+  // times as many rows.  1024 rows of 32 heads behind 7169 positions: 211 us, in blocks of 16 rows 391; six sequences of up to
+  // 700 rows of 64 heads: 121, 164.  One sequence of 500 rows and 32 heads is 64 such blocks: 34 us, in blocks of 16 rows 22.
   const int64_t many = (rows + KV4_MANY_ROWS - 1) / KV4_MANY_ROWS * p.kv_heads * r.n_seqs;
   a.many = rows > 64 && many * shares >= num_cus();
   const int block = a.many ? KV4_MANY_ROWS : KV4_FEW_ROWS;
   a.row_blocks = (int)((rows + block - 1) / block);
   a.works = (int64_t)a.row_blocks * p.kv_heads * r.n_seqs;
+  // Two workgroups a CU of the kernels for few rows (of which three or four fit), one of the other, which fills a CU's LDS.
+  // 4, 6, 9 and 16 times as many shares for few rows gained nothing: what a workgroup saves comes back in the join.
   const int64_t want = ((a.many ? 1 : 2) * num_cus() + a.works - 1) / std::max<int64_t>(a.works, 1);
   a.splits = (int)std::min<int64_t>(want, shares);
   if (a.splits > 1) a.bytes = align_up((size_t)a.works * a.splits * block * (head_dim + 2) * sizeof(float));
@@ -168,6 +172,8 @@ void kv4_launch_attention(hipStream_t s, int32_t dtype, int head_dim, const Kv4P
     auto go = [&](auto kernel) {
       hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, p, r, q, o, fresh ? *k : q, fresh ? *v : q, heads, scale, a.splits, a.row_blocks, part);
     };
+    // one query row a key head: 32 sequences of 1500 .. 2500 positions 75 us, by the kernel for up to 16 rows 93; 16 of 10 .. 560
+    // 17, 21
     if (r.max_rows == 1 && heads == p.kv_heads) {
       if (p16) fresh ? single(kv4_attn_one_kernel<T, HD, true, true>) : single(kv4_attn_one_kernel<T, HD, true, false>);
       else fresh ? single(kv4_attn_one_kernel<T, HD, false, true>) : single(kv4_attn_one_kernel<T, HD, false, false>);

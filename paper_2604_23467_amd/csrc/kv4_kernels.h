@@ -24,6 +24,7 @@ typedef u32 u32x2 __attribute__((ext_vector_type(2)));
 typedef u32 u32x4 __attribute__((ext_vector_type(4)));
 typedef u32 u32x8 __attribute__((ext_vector_type(8)));
 typedef u16 u16x8 __attribute__((ext_vector_type(8)));
+typedef u16 u16x8u __attribute__((ext_vector_type(8), aligned(2)));      // anywhere in memory: one access of 16 bytes all the same
 
 // One layer's pool
 struct Kv4Pool {
@@ -47,7 +48,6 @@ struct Kv4Rows {
 struct Kv4View {
   void* data;
   long row_stride, head_stride;
-  int wide;                  // rows of every head can be read and written 16 bytes at a time
   long layer_stride;         // from one layer to the next
   int frag_k, frag_tb;       // frag_tb > 0: rows of frag_k elements in the projections' operand order (act_offset)
 };
@@ -153,12 +153,7 @@ struct Kv4Bf16 {
   }
 };
 __device__ __forceinline__ u16x8 kv4_load8(const Kv4View& t, int row, int head, int e) {
-  const u16* p = (const u16*)t.data + row * t.row_stride + (head * t.head_stride + e);
-  if (t.wide) return *as_global(reinterpret_cast<const u16x8*>(p));
-  u16x8 v;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = *as_global(p + i);
-  return v;
+  return *(const LL_GLOBAL u16x8u*)((const u16*)t.data + row * t.row_stride + (head * t.head_stride + e));
 }
 template <int HD>
 __device__ __forceinline__ u16* kv4_element(const Kv4View& t, int row, int head, int e) {      // of an output
@@ -167,13 +162,7 @@ __device__ __forceinline__ u16* kv4_element(const Kv4View& t, int row, int head,
 }
 template <int HD>
 __device__ __forceinline__ void kv4_store8(const Kv4View& t, int row, int head, int e, u16x8 v) {
-  u16* p = kv4_element<HD>(t, row, head, e);
-  if (t.wide) {
-    *as_global(reinterpret_cast<u16x8*>(p)) = v;
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) *as_global(p + i) = v[i];
-  }
+  *(LL_GLOBAL u16x8u*)kv4_element<HD>(t, row, head, e) = v;
 }
 
 // A number that is a binary16 number of at most 8 significant bits: rounded up to the next one (x >= 0)
@@ -222,16 +211,21 @@ __device__ __forceinline__ u32 kv4_quantise(const float (&x)[8], u32& param) {
   }
   param = (u32)__builtin_bit_cast(u16, (half_t)s) | (u32)__builtin_bit_cast(u16, mid_h) << 16;
   const float inv = s > 0.f ? __builtin_amdgcn_rcpf(s) : 0.f;
-  float c[8], off = 0.f, least = fabsf(mid);
+  auto quotient = [&](float v) {
+    const float d = v - mid, y = d * inv;
+    return fmaf(fmaf(-y, s, d), inv, y);
+  };
+  float c[8], least = fabsf(mid);
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const float d = x[i] - mid, y = d * inv, q = fmaf(fmaf(-y, s, d), inv, y), n = rintf(q);
-    off = fmaxf(off, fabsf(q - n));
     least = fminf(least, fabsf(x[i]));
-    c[i] = __builtin_amdgcn_fmed3f(n, -8.f, 7.f);
+    c[i] = __builtin_amdgcn_fmed3f(rintf(quotient(x[i])), -8.f, 7.f);
   }
-  if (__any(off > 0.49999f && least < s * 0x1p-9f)) {
-    if (s > 0.f) {
+  if (__any(least < s * 0x1p-9f)) {      // (few rows get here; fewer go on)
+    float off = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) off = fmaxf(off, fabsf(quotient(x[i]) - rintf(quotient(x[i]))));
+    if (__any(off > 0.49999f && least < s * 0x1p-9f) && s > 0.f) {
 #pragma unroll 1
       for (int i = 0; i < 8; ++i) {
         float v = x[0];
@@ -249,24 +243,28 @@ __device__ __forceinline__ u32 kv4_quantise(const float (&x)[8], u32& param) {
   return four(c[0], c[1], c[2], c[3]) | four(c[4], c[5], c[6], c[7]) << 16;
 }
 
-// Rows of k and v into the cache, of several layers at once where grid.z = 2 x layers.  A thread takes 8 elements of N consecutive rows, four threads a group.  grid = (blocks of N
-// rows, parts of a row's kv_heads HD / 8 threads, keys and values).  The cache has a head's rows side by side, so the rows of a block share
-// lines of it: written one by one from different XCDs, a line of parameters (8 rows) would leave eight L2s in parts.
+// Rows of k and v into the cache, of several layers at once where grid.z = 2 x layers.  A thread takes 8 elements of N
+// consecutive rows, four threads a group.  grid = (blocks of N rows, parts of a row's kv_heads HD / 8 threads, keys and values).
+// The cache has a head's rows side by side, so the rows of a block share lines of it: written one by one from different XCDs, a
+// line of parameters (8 rows) would leave eight L2s in parts.
+// Reads 2 bytes an element and writes 5 / 8.  Four sequences of 1 .. 8190 rows of 8 heads of 128: 35 us (row by row 52), with
+// the vector unit busy half of it (25 operations an element, a quarter of them for the group's parameters) and waiting for rows the
+// rest: a thread's 8 rows are its only loads in flight.
 template <class T, int HD, int N>
 __global__ __launch_bounds__(256) void kv4_write_kernel(Kv4Pool p, Kv4Rows r, Kv4View k, Kv4View v) {
   constexpr int UPR = HD / 8;
   const int i0 = blockIdx.x * N, unit = blockIdx.y * blockDim.x + threadIdx.x, which = blockIdx.z & 1;
   const int head = unit / UPR, oct = unit % UPR;
-  int row[N];
-  kv4_places<N>(p, r, i0, row);
-  if (head >= p.kv_heads) return;
   Kv4View from = which ? v : k;
   from.data = (u16*)from.data + (blockIdx.z >> 1) * from.layer_stride;
   p.base += (blockIdx.z >> 1) * p.layer;
-  u16x8 in[N];
+  u16x8 in[N];                                         // also of rows that have no place, in front of what says so
 #pragma unroll
-  for (int n = 0; n < N; ++n)
-    if (row[n] >= 0) in[n] = kv4_load8(from, i0 + n, head, oct * 8);
+  for (int n = 0; n < N; ++n) in[n] = kv4_load8(from, min(i0 + n, r.n_rows - 1), min(head, p.kv_heads - 1), oct * 8);
+  __builtin_amdgcn_sched_barrier(0);
+  int row[N];
+  kv4_places<N>(p, r, i0, row);
+  if (head >= p.kv_heads) return;
   char *codes = kv4_codes<HD>(p, which, head) + oct * 4, *params = kv4_params<HD>(p, which, head) + oct;
 #pragma unroll
   for (int n = 0; n < N; ++n) {
@@ -286,6 +284,8 @@ __device__ __forceinline__ float kv4_value(u32 w, int i, float s, float mid) {
 }
 
 // The same rows out of the cache.  Rows of positions that are not there are zeros; grid and blocks as kv4_write_kernel's.
+// Bound by memory: 32 sequences of 1 .. 1000 rows of 32 heads of 128, 344 MB, in 74 us, 4.7 TB/s, where a copy moves 5.0 (row by
+// row: 128 us).
 template <class T, int HD, int N>
 __global__ __launch_bounds__(256) void kv4_read_kernel(Kv4Pool p, Kv4Rows r, Kv4View k, Kv4View v) {
   constexpr int UPR = HD / 8;
@@ -633,6 +633,10 @@ __device__ __forceinline__ void kv4_values(const Kv4Tile<HD>& t, const Kv4Bits& 
 // P16: page_tokens is a multiple of 16, so that halves of a tile are consecutive pool rows and their addresses scalar.
 // NEW: knew and vnew hold the sequences' last rows (one row each), which the workgroup that has the last key quantises into
 // the pool and attends from LDS.  part: with more than one split, the shares' results ([work][16][HD + 2] floats).
+// Four sequences of 30000 positions, 8 key heads of 128 and 4 query heads each: 41 us, 4.0 TB/s of the cache.  What bounds it is
+// a wave's chain of loads, codes to operands (420 vector instructions for 32 keys), products and softmax: the vector unit is
+// busy 44 % of the time, the matrix cores 8 %.  Four workgroups a CU would need 128 registers a lane, and spill: 32 sequences of
+// 2000 positions then take 125 us instead of 92.
 template <class T, int HD, bool P16, bool NEW>
 __global__ __launch_bounds__(256, 3) void kv4_attn_few_kernel(Kv4Pool p, Kv4Rows r, Kv4View q, Kv4View o, Kv4View knew, Kv4View vnew,
                                                            int heads, float scale, int splits, int row_blocks, float* part) {
@@ -923,6 +927,8 @@ __device__ __forceinline__ void kv4_barrier() {
 // a time into v_dot2_f32_f16; what 1024 and 64 add up to is taken off in front, as the start of the sum) and 2.1 for the output
 // (c - 8, then a multiply-add from a half word to 32 bits).  HD / 32 lanes hold a key, a group of 32 elements each, so that a lane
 // has one step and one middle.  All of a wave's lanes share the running maximum; weights stay in 32 bits.
+// 32 sequences of 1500 .. 2500 positions of 32 heads: 69 us, 4.8 TB/s of the cache; a kernel that only loads the same bytes in
+// this pattern takes 57 .. 60, whatever the loads' width.
 #define KV4_ONE_STEPS 2          // keys of a lane in a trip: 4 of them leave registers for three workgroups a CU only (77 -> 79 us)
 
 template <class T, int HD, bool P16, bool NEW>
@@ -1206,7 +1212,12 @@ __global__ __launch_bounds__(256, 4) void kv4_attn_one_kernel(Kv4Pool p, Kv4Rows
 //  * S^T leaves the lane with keys 8 a + 4 h + b (a, b < 4) of query c; product n of V^T P^T contracts over a = 2 n and 2 n + 1;
 //  * V: row c of block e is element (HD / 32) c + e, and the lane's outputs are HD / 8 elements in a row for every a, of group a
 //    (head_dim 64: a / 2).  Rows of the further block: 4 x the group's middle, 4 x + 1 ones, 4 x + 2 the group's NaN marks.
-// Weights enter as one binary16 number here: their rounding is as large as that of a binary16 output.
+// Weights enter as one binary16 number here: a relative 2^-11 each, independent of the others', as large as a binary16 output's
+// own rounding; a second one would be another KV4_MANY_ROWS x keys x head_dim product.
+// 1024 rows of 32 heads behind 7169 positions: 190 us and a join of 20, 0.61 PFLOP/s of 1.15 that a large library product
+// reaches; blocks of 128 rows took 205 and 20.  The vector unit (weights, operands) is busy 43 % of the time, the matrix cores
+// 31 %, and a wave reads 19 KB of LDS for 32 keys; they overlap only across a SIMD's two waves.  64 rows a wave, which would
+// halve the LDS reads, needs more than a lane's 512 registers: 532 us with the spills.
 #define KV4_MANY_ROWS 256
 #define KV4_MANY_WAVES 8
 
@@ -1512,7 +1523,8 @@ __global__ __launch_bounds__(KV4_MANY_WAVES * 64, 2) void kv4_attn_many_kernel(K
 }
 
 // The shares of a query row together: a wave a row, a lane a share for the weights, then HD / 64 elements a lane.
-// grid = (kv_heads * row blocks * sequences, ROWS / 4)
+// grid = (kv_heads * row blocks * sequences, ROWS / 4).  Bound by its chain of loads: 4.7 us for 256 rows of 8 shares (10.5 with
+// a workgroup a row block), 20 us where it reads 32768 rows of 2 shares, 34 MB.
 template <class T, int HD, int ROWS>
 __global__ __launch_bounds__(256) void kv4_join_kernel(Kv4Pool p, Kv4Rows r, Kv4View o, int heads, int splits, int row_blocks,
                                                        const float* part) {

@@ -1437,8 +1437,8 @@ void enqueue_batch_step(Instance* I, hipStream_t s) {
       Kv4Rows r{};
       r.len = bs->pos; r.len_add = 1; r.active = bs->active; r.order = bs->order; r.table = table;
       r.n_seqs = r.n_rows = Mb; r.max_rows = 1; r.table_stride = B->L.pt_stride;
-      const Kv4View q{Qh, d, c.head_dim, 1, 0, 0, 0}, k{fresh, c.head_dim, (long)Mb * c.head_dim, 1, 0, 0, 0},
-          v{fresh + fresh_v, c.head_dim, (long)Mb * c.head_dim, 1, 0, 0, 0}, o{Oh, 0, 0, 1, 0, d, tb};
+      const Kv4View q{Qh, d, c.head_dim, 0, 0, 0}, k{fresh, c.head_dim, (long)Mb * c.head_dim, 0, 0, 0},
+          v{fresh + fresh_v, c.head_dim, (long)Mb * c.head_dim, 0, 0, 0}, o{Oh, 0, 0, 0, d, tb};
       kv4_launch_attention(s, LL_F16, c.head_dim, B->kv4(l), r, c.n_heads, 1.0f / sqrtf((float)c.head_dim), q, &k, &v, o, B->L.plan,
                            B->at<float>(B->L.part));
       a.rows_apart = 0;
@@ -2073,7 +2073,7 @@ int32_t ll_batch_add(const int32_t* tokens, int32_t n, int32_t* first_token) {
       Kv4Rows r{};
       r.len = B->at<BatchState>(B->L.state)->pos + slot; r.table = B->at<int>(B->L.page_table) + (size_t)slot * B->L.pt_stride;
       r.n_seqs = 1; r.max_rows = r.n_rows = n; r.table_stride = B->L.pt_stride;
-      const Kv4View k{I->kcache(0), c.head_dim, (long)c.max_seq * c.head_dim, 1, 2 * (long)I->L.kv_layer_halves, 0, 0};
+      const Kv4View k{I->kcache(0), c.head_dim, (long)c.max_seq * c.head_dim, 2 * (long)I->L.kv_layer_halves, 0, 0};
       Kv4View v = k;
       v.data = I->vcache(0);
       kv4_launch_write(I->stream, LL_F16, c.head_dim, B->kv4(0), r, k, v, c.n_layers);
@@ -2212,7 +2212,7 @@ int ll_batch_dbg_get_kv(int32_t slot, int32_t layer, int32_t which, int32_t n_po
       r.len = B->at<BatchState>(B->L.state)->pos + slot; r.len_add = p0 + m - B->h_state->pos[slot];
       r.table = B->at<int>(B->L.page_table) + (size_t)slot * B->L.pt_stride;
       r.n_seqs = 1; r.max_rows = r.n_rows = m; r.table_stride = B->L.pt_stride;
-      const Kv4View k{rows, d, c.head_dim, 1, 0, 0, 0}, v{rows + (size_t)m * d, d, c.head_dim, 1, 0, 0, 0};
+      const Kv4View k{rows, d, c.head_dim, 0, 0, 0}, v{rows + (size_t)m * d, d, c.head_dim, 0, 0, 0};
       kv4_launch_read(I->stream, LL_F16, c.head_dim, B->kv4(layer), r, k, v);
       HIPCHK(hipGetLastError());
       HIPCHK(hipStreamSynchronize(I->stream));
