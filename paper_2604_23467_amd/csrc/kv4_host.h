@@ -88,8 +88,8 @@ void kv4_dispatch(int32_t dtype, int head_dim, F&& go) {
   else head_dim == 128 ? go(Kv4Bf16{}, Kv4Dim<128>{}) : go(Kv4Bf16{}, Kv4Dim<64>{});
 }
 
-// Blocks of 8 rows where they still give every CU two workgroups: reading 32 x 1 .. 1000 rows of 32 heads takes 83 us, row by
-// row 134; writing 4 x 1 .. 8190 rows of 8 heads and reading them 64, row by row 67.  Single rows, whose chain is shorter, else:
+// Blocks of 8 rows where they still give every CU two workgroups: reading 32 x 1 .. 1000 rows of 32 heads takes 77 us, row by
+// row 134; writing 4 x 1 .. 8190 rows of 8 heads and reading them 61, row by row 67.  Single rows, whose chain is shorter, else:
 // writing 16 rows 7.6 us, in blocks 15.3; 500 rows of 32 heads and reading them 13.8, 18.4.
 constexpr int kKv4RowBlock = 8;
 template <class F>

@@ -247,9 +247,9 @@ __device__ __forceinline__ u32 kv4_quantise(const float (&x)[8], u32& param) {
 // consecutive rows, four threads a group.  grid = (blocks of N rows, parts of a row's kv_heads HD / 8 threads, keys and values).
 // The cache has a head's rows side by side, so the rows of a block share lines of it: written one by one from different XCDs, a
 // line of parameters (8 rows) would leave eight L2s in parts.
-// Reads 2 bytes an element and writes 5 / 8.  Four sequences of 1 .. 8190 rows of 8 heads of 128: 35 us (row by row 52), with
-// the vector unit busy half of it (25 operations an element, a quarter of them for the group's parameters) and waiting for rows the
-// rest: a thread's 8 rows are its only loads in flight.
+// Reads 2 bytes an element and writes 5 / 8.  Four sequences of 1 .. 8190 rows of 8 heads of 128: 34 us (row by row 52), with
+// the vector unit busy half of it (23 operations an element, a quarter of them for the group's parameters) and waiting for memory
+// the rest: rows are requested in front of the look-up of their places, which takes three dependent loads (behind it: 35 us).
 template <class T, int HD, int N>
 __global__ __launch_bounds__(256) void kv4_write_kernel(Kv4Pool p, Kv4Rows r, Kv4View k, Kv4View v) {
   constexpr int UPR = HD / 8;
@@ -635,7 +635,7 @@ __device__ __forceinline__ void kv4_values(const Kv4Tile<HD>& t, const Kv4Bits& 
 // the pool and attends from LDS.  part: with more than one split, the shares' results ([work][16][HD + 2] floats).
 // Four sequences of 30000 positions, 8 key heads of 128 and 4 query heads each: 41 us, 4.0 TB/s of the cache.  What bounds it is
 // a wave's chain of loads, codes to operands (420 vector instructions for 32 keys), products and softmax: the vector unit is
-// busy 44 % of the time, the matrix cores 8 %.  Four workgroups a CU would need 128 registers a lane, and spill: 32 sequences of
+// busy 46 % of the time, the matrix cores 9 %.  Four workgroups a CU would need 128 registers a lane, and spill: 32 sequences of
 // 2000 positions then take 125 us instead of 92.
 template <class T, int HD, bool P16, bool NEW>
 __global__ __launch_bounds__(256, 3) void kv4_attn_few_kernel(Kv4Pool p, Kv4Rows r, Kv4View q, Kv4View o, Kv4View knew, Kv4View vnew,
@@ -927,7 +927,7 @@ __device__ __forceinline__ void kv4_barrier() {
 // a time into v_dot2_f32_f16; what 1024 and 64 add up to is taken off in front, as the start of the sum) and 2.1 for the output
 // (c - 8, then a multiply-add from a half word to 32 bits).  HD / 32 lanes hold a key, a group of 32 elements each, so that a lane
 // has one step and one middle.  All of a wave's lanes share the running maximum; weights stay in 32 bits.
-// 32 sequences of 1500 .. 2500 positions of 32 heads: 69 us, 4.8 TB/s of the cache; a kernel that only loads the same bytes in
+// 32 sequences of 1500 .. 2500 positions of 32 heads: 67 us, 4.9 TB/s of the cache; a kernel that only loads the same bytes in
 // this pattern takes 57 .. 60, whatever the loads' width.
 #define KV4_ONE_STEPS 2          // keys of a lane in a trip: 4 of them leave registers for three workgroups a CU only (77 -> 79 us)
 
@@ -1215,8 +1215,8 @@ __global__ __launch_bounds__(256, 4) void kv4_attn_one_kernel(Kv4Pool p, Kv4Rows
 // Weights enter as one binary16 number here: a relative 2^-11 each, independent of the others', as large as a binary16 output's
 // own rounding; a second one would be another KV4_MANY_ROWS x keys x head_dim product.
 // 1024 rows of 32 heads behind 7169 positions: 190 us and a join of 20, 0.61 PFLOP/s of 1.15 that a large library product
-// reaches; blocks of 128 rows took 205 and 20.  The vector unit (weights, operands) is busy 43 % of the time, the matrix cores
-// 31 %, and a wave reads 19 KB of LDS for 32 keys; they overlap only across a SIMD's two waves.  64 rows a wave, which would
+// reaches; blocks of 128 rows took 205 and 20.  The vector unit (weights, operands) is busy 44 % of the time, the matrix cores
+// 32 %, and a wave reads 19 KB of LDS for 32 keys; they overlap only across a SIMD's two waves.  64 rows a wave, which would
 // halve the LDS reads, needs more than a lane's 512 registers: 532 us with the spills.
 #define KV4_MANY_ROWS 256
 #define KV4_MANY_WAVES 8
