@@ -346,7 +346,7 @@ def ll_kv4_read(cache, rows, k=None, v=None, n_rows=0, dtype=None, stream=None):
     heads = cache.n_kv_heads
     if k is None:
         k = torch.empty((n_rows, heads, cache.head_dim), dtype=dtype, device=cache.device)
-        v = torch.empty((n_rows, heads, cache.head_dim), dtype=dtype, device=cache.device)
+        v = torch.empty_like(k)
     rc = load().ll_kv4_read(cache.c, rows.c, kind, _kv4_view(k, "k", cache, heads, n_rows, dtype),
                             _kv4_view(v, "v", cache, heads, n_rows, dtype), s)
     if rc < 0:
@@ -376,7 +376,7 @@ def ll_kv4_attention(cache, rows, q, k=None, v=None, scale=0.0, out=None, worksp
     kv = None if k is None else _kv4_view(k, "k", cache, cache.n_kv_heads, n, dtype)
     vv = None if v is None else _kv4_view(v, "v", cache, cache.n_kv_heads, n, dtype)
     if out is None:
-        out = torch.empty(shape, dtype=dtype, device=cache.device)
+        out = q.new_empty(shape)
     ov = _kv4_view(out, "out", cache, heads, n, dtype)
     lib = load()
     if workspace is None:

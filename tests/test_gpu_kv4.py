@@ -244,6 +244,12 @@ def test_layouts_of_rows(ll, layout, head_dim):
     attend(ll, "bf16", 4, 2, head_dim, 16, [30, 1, 70], [30, 40, 300], layout=layout, new=True)
 
 
+@pytest.mark.parametrize("head_dim", [64, 128])
+def test_odd_addresses_in_the_kernels_for_one_and_for_many_rows(ll, head_dim):
+    attend(ll, "f16", 3, 3, head_dim, 16, [1, 1, 1], [5, 40, 300], layout="odd", ragged=False, new=True)
+    attend(ll, "bf16", 32, 32, head_dim, 16, [65] * 8, [65, 66, 70, 80, 90, 100, 110, 120], layout="odd", ragged=False)
+
+
 def test_pages_that_are_not_there(ll):
     """Positions without a page are seen by nobody; a row that then sees nothing gives zeros."""
     out = attend(ll, "f16", 2, 2, 128, 16, [1, 1, 1], [100, 20, 40], ragged=False, holes=[(0, 0), (0, 3), (1, 0), (1, 1), (2, 2)])
