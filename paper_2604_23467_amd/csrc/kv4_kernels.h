@@ -1530,6 +1530,7 @@ __global__ __launch_bounds__(256) void kv4_join_kernel(Kv4Pool p, Kv4Rows r, Kv4
                                                        const float* part) {
   typedef float vec __attribute__((ext_vector_type(HD / 64)));
   constexpr size_t PART = ROWS * (HD + 2);
+  constexpr int B = ROWS > KV4_FEW_ROWS ? 2 : 16;       // shares requested at once
   Kv4Work w = kv4_work(r, blockIdx.x, 1, p.kv_heads, row_blocks);
   if (ROWS > KV4_FEW_ROWS) w.rb = row_blocks - 1 - w.rb;
   const Kv4Seq s = kv4_seq(r, w.b);
@@ -1541,7 +1542,14 @@ __global__ __launch_bounds__(256) void kv4_join_kernel(Kv4Pool p, Kv4Rows r, Kv4
   const int tiles = (n_keys + KV4_TILE - 1) / KV4_TILE, share = kv4_share(tiles, splits);
   const int n = tiles ? (tiles + share - 1) / share : 1;
   const float* from = part + (size_t)blockIdx.x * splits * PART;
+  const float* at = from + row * HD + lane * (HD / 64);
+  vec v[B];
+  auto load = [&](int k) {
+#pragma unroll
+    for (int i = 0; i < B; ++i) v[i] = *as_global(reinterpret_cast<const vec*>(at + min(k + i, n - 1) * PART));
+  };
   const float m = lane < n ? from[lane * PART + ROWS * HD + row] : -INFINITY, l = lane < n ? from[lane * PART + ROWS * HD + ROWS + row] : 0.f;
+  load(0);
   float top = m;
 #pragma unroll
   for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
@@ -1549,14 +1557,12 @@ __global__ __launch_bounds__(256) void kv4_join_kernel(Kv4Pool p, Kv4Rows r, Kv4
   const float sum = wave_sum(weight * l);
   const float inv = sum != 0.f ? 1.0f / sum : 0.f;
   vec a{};
-  const float* at = from + row * HD + lane * (HD / 64);
-  for (int k = 0; k < n; k += 8) {
-    vec v[8];
+  for (int k = 0;;) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = *as_global(reinterpret_cast<const vec*>(at + min(k + i, n - 1) * PART));
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
+    for (int i = 0; i < B; ++i)
       if (k + i < n) a += v[i] * __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, weight), k + i));
+    if ((k += B) >= n) break;
+    load(k);
   }
   const int j = f / share_heads;
   u16* to = kv4_element<HD>(o, s.first + j, w.head * share_heads + f - j * share_heads, lane * (HD / 64));
