@@ -132,7 +132,7 @@ Kv4Plan kv4_plan(const Kv4Pool& p, const Kv4Rows& r, int max_len, int head_dim, 
   const int64_t rounds = (len + KV4_TILE * KV4_WAVES - 1) / (KV4_TILE * KV4_WAVES);      // of the four waves over the keys
   const int64_t shares = std::max<int64_t>(1, std::min<int64_t>(rounds / 4, 64));        // at most (64: a wave's lanes, see the join)
   // Blocks of 256 rows where they, times the shares, leave no CU idle: there a workgroup turns codes into operands once for 16
-  // times as many rows.  1024 rows of 32 heads behind 7169 positions: 211 us, in blocks of 16 rows 391; six sequences of up to
+  // times as many rows.  1024 rows of 32 heads behind 7169 positions: 204 us, in blocks of 16 rows 391; six sequences of up to
   // 700 rows of 64 heads: 121, 164.  One sequence of 500 rows and 32 heads is 64 such blocks: 34 us, in blocks of 16 rows 22.
   const int64_t many = (rows + KV4_MANY_ROWS - 1) / KV4_MANY_ROWS * p.kv_heads * r.n_seqs;
   a.many = rows > 64 && many * shares >= num_cus();
@@ -162,7 +162,7 @@ void kv4_launch_attention(hipStream_t s, int32_t dtype, int head_dim, const Kv4P
       };
       p16 ? go(kv4_attn_many_kernel<T, HD, true>) : go(kv4_attn_many_kernel<T, HD, false>);
       if (a.splits > 1)
-        hipLaunchKernelGGL((kv4_join_kernel<T, HD, KV4_MANY_ROWS>), dim3((unsigned)a.works, KV4_MANY_ROWS / 4), dim3(256), 0, s, p, r, o,
+        hipLaunchKernelGGL((kv4_join_kernel<T, HD, KV4_MANY_ROWS>), dim3((unsigned)a.works, KV4_MANY_ROWS / 4 / KV4_JOIN_ROWS(KV4_MANY_ROWS)), dim3(256), 0, s, p, r, o,
                            heads, a.splits, a.row_blocks, part);
       return;
     }
@@ -180,7 +180,7 @@ void kv4_launch_attention(hipStream_t s, int32_t dtype, int head_dim, const Kv4P
     } else if (p16) fresh ? go(kv4_attn_few_kernel<T, HD, true, true>) : go(kv4_attn_few_kernel<T, HD, true, false>);
     else fresh ? go(kv4_attn_few_kernel<T, HD, false, true>) : go(kv4_attn_few_kernel<T, HD, false, false>);
     if (a.splits > 1)
-      hipLaunchKernelGGL((kv4_join_kernel<T, HD, KV4_FEW_ROWS>), dim3((unsigned)a.works, KV4_FEW_ROWS / 4), dim3(256), 0, s, p, r, o, heads,
+      hipLaunchKernelGGL((kv4_join_kernel<T, HD, KV4_FEW_ROWS>), dim3((unsigned)a.works, KV4_FEW_ROWS / 4 / KV4_JOIN_ROWS(KV4_FEW_ROWS)), dim3(256), 0, s, p, r, o, heads,
                          a.splits, a.row_blocks, part);
   });
 }

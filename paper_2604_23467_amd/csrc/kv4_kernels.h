@@ -1214,8 +1214,8 @@ __global__ __launch_bounds__(256, 4) void kv4_attn_one_kernel(Kv4Pool p, Kv4Rows
 //    (head_dim 64: a / 2).  Rows of the further block: 4 x the group's middle, 4 x + 1 ones, 4 x + 2 the group's NaN marks.
 // Weights enter as one binary16 number here: a relative 2^-11 each, independent of the others', as large as a binary16 output's
 // own rounding; a second one would be another KV4_MANY_ROWS x keys x head_dim product.
-// 1024 rows of 32 heads behind 7169 positions: 190 us and a join of 20, 0.61 PFLOP/s of 1.15 that a large library product
-// reaches; blocks of 128 rows took 205 and 20.  The vector unit (weights, operands) is busy 44 % of the time, the matrix cores
+// 1024 rows of 32 heads behind 7169 positions: 190 us and a join of 12, 0.64 PFLOP/s of 1.15 that a large library product
+// reaches; blocks of 128 rows took 205.  The vector unit (weights, operands) is busy 44 % of the time, the matrix cores
 // 32 %, and a wave reads 19 KB of LDS for 32 keys; they overlap only across a SIMD's two waves.  64 rows a wave, which would
 // halve the LDS reads, needs more than a lane's 512 registers: 532 us with the spills.
 #define KV4_MANY_ROWS 256
@@ -1522,50 +1522,70 @@ __global__ __launch_bounds__(KV4_MANY_WAVES * 64, 2) void kv4_attn_many_kernel(K
   }
 }
 
-// The shares of a query row together: a wave a row, a lane a share for the weights, then HD / 64 elements a lane.
-// grid = (kv_heads * row blocks * sequences, ROWS / 4).  Bound by its chain of loads: 4.7 us for 256 rows of 8 shares (10.5 with
-// a workgroup a row block), 20 us where it reads 32768 rows of 2 shares, 34 MB.
+// The shares of a query row together: a wave a row (of many rows: four), a lane a share for the weights, then HD / 64 elements a
+// lane.  grid = (kv_heads * row blocks * sequences, ROWS / 4 / rows of a wave).
+// Rows of a block that the sequence has not got are read, within the block's part, and not used.
+// Bound by its chain (place, shares' maxima, store) and, for many rows, by the instructions around 16 bytes a lane: 32768 rows
+// of 2 shares, 34 MB, 12 us (a wave a row, requested in front of the weights 18.6, behind them 20.4); 128 rows of 16 shares 4.7
+// (a workgroup a row block: 10.5).
+#define KV4_JOIN_ROWS(block) ((block) > KV4_FEW_ROWS ? 4 : 1)
 template <class T, int HD, int ROWS>
 __global__ __launch_bounds__(256) void kv4_join_kernel(Kv4Pool p, Kv4Rows r, Kv4View o, int heads, int splits, int row_blocks,
                                                        const float* part) {
   typedef float vec __attribute__((ext_vector_type(HD / 64)));
   constexpr size_t PART = ROWS * (HD + 2);
-  constexpr int B = ROWS > KV4_FEW_ROWS ? 2 : 16;       // shares requested at once
+  constexpr int R = KV4_JOIN_ROWS(ROWS), B = ROWS > KV4_FEW_ROWS ? 2 : 16;      // rows of a wave, shares requested at once
   Kv4Work w = kv4_work(r, blockIdx.x, 1, p.kv_heads, row_blocks);
   if (ROWS > KV4_FEW_ROWS) w.rb = row_blocks - 1 - w.rb;
   const Kv4Seq s = kv4_seq(r, w.b);
   const int share_heads = heads / p.kv_heads, rows = min(s.rows, r.max_rows) * share_heads;
-  const int lane = threadIdx.x & 63, row = blockIdx.y * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int f0 = w.rb * ROWS, f = f0 + row;
-  if (f >= rows) return;
+  const int lane = threadIdx.x & 63, row0 = (blockIdx.y * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * R;
+  const int f0 = w.rb * ROWS;
+  if (f0 + row0 >= rows) return;
   const int n_keys = kv4_keys(p, r, s, min(f0 + ROWS - 1, rows - 1) / share_heads);
   const int tiles = (n_keys + KV4_TILE - 1) / KV4_TILE, share = kv4_share(tiles, splits);
   const int n = tiles ? (tiles + share - 1) / share : 1;
   const float* from = part + (size_t)blockIdx.x * splits * PART;
-  const float* at = from + row * HD + lane * (HD / 64);
-  vec v[B];
+  vec v[R][B], a[R];
+  float m[R], weight[R], inv[R];
   auto load = [&](int k) {
 #pragma unroll
-    for (int i = 0; i < B; ++i) v[i] = *as_global(reinterpret_cast<const vec*>(at + min(k + i, n - 1) * PART));
-  };
-  const float m = lane < n ? from[lane * PART + ROWS * HD + row] : -INFINITY, l = lane < n ? from[lane * PART + ROWS * HD + ROWS + row] : 0.f;
-  load(0);
-  float top = m;
+    for (int q = 0; q < R; ++q)
 #pragma unroll
-  for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-  const float weight = m > -INFINITY ? __builtin_amdgcn_exp2f(m - top) : 0.f;
-  const float sum = wave_sum(weight * l);
-  const float inv = sum != 0.f ? 1.0f / sum : 0.f;
-  vec a{};
+      for (int i = 0; i < B; ++i)
+        v[q][i] = *as_global(reinterpret_cast<const vec*>(from + (row0 + q) * HD + lane * (HD / 64) + min(k + i, n - 1) * PART));
+  };
+#pragma unroll
+  for (int q = 0; q < R; ++q) {
+    m[q] = lane < n ? from[lane * PART + ROWS * HD + row0 + q] : -INFINITY;
+    inv[q] = lane < n ? from[lane * PART + ROWS * HD + ROWS + row0 + q] : 0.f;
+  }
+  load(0);
+#pragma unroll
+  for (int q = 0; q < R; ++q) {
+    float top = m[q];
+#pragma unroll
+    for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+    weight[q] = m[q] > -INFINITY ? __builtin_amdgcn_exp2f(m[q] - top) : 0.f;
+    const float sum = wave_sum(weight[q] * inv[q]);
+    inv[q] = sum != 0.f ? 1.0f / sum : 0.f;
+    a[q] = vec{};
+  }
   for (int k = 0;;) {
 #pragma unroll
-    for (int i = 0; i < B; ++i)
-      if (k + i < n) a += v[i] * __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, weight), k + i));
+    for (int q = 0; q < R; ++q)
+#pragma unroll
+      for (int i = 0; i < B; ++i)
+        if (k + i < n) a[q] += v[q][i] * __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, weight[q]), k + i));
     if ((k += B) >= n) break;
     load(k);
   }
-  const int j = f / share_heads;
-  u16* to = kv4_element<HD>(o, s.first + j, w.head * share_heads + f - j * share_heads, lane * (HD / 64));
 #pragma unroll
-  for (int i = 0; i < HD / 64; ++i) to[i] = T::store(a[i] * inv);
+  for (int q = 0; q < R; ++q) {
+    const int f = f0 + row0 + q, j = f / share_heads;
+    if (f >= rows) break;
+    u16* to = kv4_element<HD>(o, s.first + j, w.head * share_heads + f - j * share_heads, lane * (HD / 64));
+#pragma unroll
+    for (int i = 0; i < HD / 64; ++i) to[i] = T::store(a[q][i] * inv[q]);
+  }
 }
